@@ -501,6 +501,190 @@ LRC_API lrc_status lrc_tt_left_orthogonalize(double* const* cores, const int64_t
  */
 LRC_API lrc_status lrc_probe_peak(int kind, int64_t iters, double* flops_out, lrc_stream_t stream);
 
+/*
+ * 4-bit matrices -- the remainder of a rank-compensated layer: a matrix kept
+ * as 4-bit codes with a scale per row and group of columns, beside the
+ * low-rank factors that lrc_apply applies.  Entry (i, c) of an m x n matrix
+ * stands for
+ *
+ *     What[i][c] = scale[c / group][i] * (code[i][c] - zero[c / group][i]),
+ *
+ * with codes 0 ... 15 and zero = 8 where there are no zero codes.
+ *
+ *   Q       device, m rows of lrc_q4_row_bytes(n) bytes: 64-byte blocks of 128
+ *           columns.  In a block, column 32 j + 8 t + e (j, t < 4, e < 8) is in
+ *           the little-endian 32-bit word 4 t + j, at the four bits from
+ *           4 p[e] on, p = {0, 4, 1, 5, 2, 6, 3, 7}.  (The order in which the
+ *           product's matrix instructions take the columns, so that a thread
+ *           loads 16 bytes at once for any group.)  Codes of columns beyond n
+ *           may hold anything
+ *   scales  device, ceil(n / group) rows of lrc_packed_ld(m) elements: one row
+ *           per group of columns, LRC_F32 -> binary32, LRC_F16 and LRC_F16_O16
+ *           -> binary16, LRC_BF16 -> bfloat16
+ *   zeros   device, the same shape in bytes, or NULL; values 0 ... 15
+ *   group   columns that share a scale: 32, 64 or 128, else
+ *           LRC_ERR_UNSUPPORTED (LRC_F64 too)
+ *
+ * Q, scales and zeros are 16-byte aligned.
+ */
+LRC_API int64_t lrc_q4_row_bytes(int64_t n);   /* 64 ceil(n / 128); -1 for n < 0 */
+
+/*
+ * lrc_q4_round -- rounds a matrix to 4-bit codes.
+ *
+ *   W       device, m x n, row pitch ldw (>= n), format `wfmt` (LRC_F64 is
+ *           rounded to binary32 first); aligned to its element size
+ *   Q, scales, zeros, group, fmt   as above, written (pad columns get the code
+ *           of zero; scales and zeros beyond row m are not written); zeros
+ *           may be NULL
+ *
+ * With binary32 arithmetic, each operation rounded to nearest even:
+ * without zeros, s = max|w| (1/7) over the group; with zeros, lo = min(w, 0),
+ * hi = max(w, 0), s = (hi - lo) (1/15), where 1/7 and 1/15 are the binary32
+ * numbers next to them.  s is lowered to the largest finite number of `fmt`,
+ * rounded to `fmt`, and set to 0 where it is below 2^-126; v = 1 / s (0 where
+ * s = 0).  zero = 8, or rint(-lo v) kept in 0 ... 15; code = rint(w v) + zero
+ * kept in 0 ... 15 (rint: ties to even).  A group that holds an infinity or a
+ * NaN gets a NaN scale and codes and zero 8, so that its rows' products show it.
+ * Asynchronous on `stream`.
+ */
+LRC_API lrc_status lrc_q4_round(const void* W, lrc_fmt wfmt, int64_t m, int64_t n, int64_t ldw, void* Q, void* scales,
+                                uint8_t* zeros, int64_t group, lrc_fmt fmt, lrc_stream_t stream);
+
+/*
+ * lrc_q4_widen -- the values that a 4-bit matrix stands for, for eta
+ * (lrc_fro_diff) or for a dense product.
+ *
+ *   dst     device, m x n, row pitch ld_dst (>= n), format `dfmt`; aligned to
+ *           its element size; columns [n, ld_dst) are not written
+ *
+ * scale (code - zero) is formed in binary64 for LRC_F64 (exact), else in
+ * binary32, and rounded once to a 16-bit dfmt.  Asynchronous on `stream`.
+ */
+LRC_API lrc_status lrc_q4_widen(const void* Q, const void* scales, const uint8_t* zeros, int64_t group, lrc_fmt fmt,
+                                int64_t m, int64_t n, void* dst, lrc_fmt dfmt, int64_t ld_dst, lrc_stream_t stream);
+
+/*
+ * lrc_q4_apply -- product of a 4-bit matrix with b vectors:
+ *
+ *     Y = A + X What^T.
+ *
+ *   X       device, b x n, one vector per row, row pitch lrc_packed_ld(n); pad
+ *           columns are never read
+ *   A       device, b x m, row pitch m, the type of Y; NULL for none.  May be
+ *           Y itself: Y += X What^T, on top of an lrc_apply into the same Y
+ *   Y       device, b x m, row pitch m
+ *   b       >= 0 (0: nothing is launched)
+ *
+ * Element types of X and Y as in lrc_apply (LRC_F32, LRC_F32_TC: binary32;
+ * LRC_F16: binary16 and binary32; LRC_F16_O16, LRC_BF16: 16 bits both); X, A
+ * and Y 16-byte aligned.  Products with the integers code - zero are exact and
+ * are summed in binary32 over at most a group of columns; each such sum is
+ * scaled and added in binary32; A is added and the result rounded to Y's type
+ * once.  (A group's sum comes before its scale: entries of X above 2^115 could
+ * overflow there.)  Deterministic.  Made for the few vectors of a serving step:
+ * the weights are read once for up to 64 of them.  Asynchronous on `stream`.
+ */
+LRC_API lrc_status lrc_q4_apply(const void* Q, const void* scales, const uint8_t* zeros, const void* X, const void* A,
+                                void* Y, int64_t m, int64_t n, int64_t b, int64_t group, lrc_fmt fmt,
+                                lrc_stream_t stream);
+
+/*
+ * lrc_layer_norm -- layer norm of each row of X:
+ *
+ *     mu = mean(x), r = (mean((x - mu)^2) + eps)^(-1/2),
+ *     y = (x - mu) r gamma + beta.
+ *
+ *   X       device, rows x cols, row pitch ldx (>= cols), storage type of `fmt`
+ *   gamma, beta   device, cols values of type `pfmt`: LRC_F32, or a format of
+ *           X's storage type; NULL for ones and zeros
+ *   Y       device, rows x cols, row pitch ldy (>= cols), output type of `fmt`
+ *           (LRC_F32: binary32; LRC_F16: binary16 to binary32; LRC_F16_O16,
+ *           LRC_BF16: 16 bits).  May be X where type and pitch are the same
+ *   mean, rstd    device, rows binary32 values mu and r, for the gradient; NULL
+ *           where they are not wanted
+ *   rows    >= 0 (0: nothing is launched); cols >= 1; eps >= 0 and finite
+ *
+ * Columns beyond cols are neither read nor written.  Every pointer is aligned
+ * to its element size.  All arithmetic is binary32: the mean first, then the
+ * squares of x - mu.  A row of one value, or of equal ones, with eps = 0 has
+ * r = infinity and gives NaN.  LRC_F64 is LRC_ERR_UNSUPPORTED.  Deterministic.
+ * Asynchronous on `stream`.
+ */
+LRC_API lrc_status lrc_layer_norm(const void* X, const void* gamma, const void* beta, void* Y, float* mean, float* rstd,
+                                  int64_t rows, int64_t cols, int64_t ldx, int64_t ldy, double eps, lrc_fmt fmt,
+                                  lrc_fmt pfmt, lrc_stream_t stream);
+
+/*
+ * lrc_layer_norm_grad -- its gradient: with d = dy gamma and xh = (x - mu) r,
+ *
+ *     dx = r (d - mean(d) - xh mean(d xh)),
+ *     dgamma = sum over the rows of dy xh,  dbeta = sum over the rows of dy.
+ *
+ *   dY      device, rows x cols, row pitch lddy, output type of `fmt`
+ *   X, gamma, mean, rstd   as lrc_layer_norm took and gave them
+ *   dX      device, rows x cols, row pitch lddx, storage type of `fmt`; NULL
+ *           where it is not wanted.  May be X, or dY where type and pitch are
+ *           the same
+ *   dgamma, dbeta   device, cols binary32 values, written (not added to); NULL
+ *           where they are not wanted.  rows = 0 gives zeros
+ *
+ * All arithmetic is binary32.  The sums over the rows go through partial sums
+ * in the stream's workspace (see lrc_apply), added in a fixed order:
+ * deterministic.  Asynchronous on `stream`.
+ */
+LRC_API lrc_status lrc_layer_norm_grad(const void* dY, const void* X, const void* gamma, const float* mean,
+                                       const float* rstd, void* dX, float* dgamma, float* dbeta, int64_t rows,
+                                       int64_t cols, int64_t lddy, int64_t ldx, int64_t lddx, lrc_fmt fmt, lrc_fmt pfmt,
+                                       lrc_stream_t stream);
+
+/*
+ * lrc_distill -- distillation loss of logits against a teacher's top logits,
+ * and its gradient: for each row, with q = softmax(z / tau) over all V logits
+ * and p = softmax(t / tau) over the row's teacher entries,
+ *
+ *     loss = tau^2 w sum_k p_k (log p_k - log q_{i_k}),
+ *     dz_j = tau w (q_j - sum over k with i_k = j of p_k).
+ *
+ *   Z       device, rows x V logits, row pitch ldz (>= V), storage type of `fmt`
+ *   T, idx  device, rows x K teacher logits (row pitch ldt >= K, storage type
+ *           of `tfmt`) and their places in the row, int64, row pitch ldt.  An
+ *           entry with an index outside [0, V) is absent, as is one with the
+ *           logit -infinity.  The same place may be named more than once.
+ *           1 <= K <= 1024, else LRC_ERR_UNSUPPORTED
+ *   w       device, rows binary32 weights; NULL for ones
+ *   loss    device, rows binary32 values; NULL where not wanted
+ *   lse     device, rows binary32 values log sum_j exp(z_j / tau); NULL where
+ *           not wanted
+ *   dZ      device, rows x V, row pitch lddz (>= V), Z's type; NULL where not
+ *           wanted.  May be Z where the pitch is the same
+ *   tau     > 0 and finite
+ *
+ * A row without teacher entries, or with w = 0, has loss 0 and gradient 0,
+ * whatever its logits are.  Logits of -infinity have q = 0 (a teacher entry
+ * there makes the loss infinite); a row that has only those, or a NaN or
+ * +infinity, gives NaN.  All pointers are aligned to their element size.
+ * Z is read from memory once.  Arithmetic is binary32; dZ is rounded once.
+ * LRC_F64 is LRC_ERR_UNSUPPORTED.  rows = 0: nothing is launched.
+ * Deterministic.  Asynchronous on `stream`.
+ */
+LRC_API lrc_status lrc_distill(const void* Z, const void* T, const int64_t* idx, const float* w, float* loss, float* lse,
+                               void* dZ, int64_t rows, int64_t V, int64_t K, int64_t ldz, int64_t ldt, int64_t lddz,
+                               double tau, lrc_fmt fmt, lrc_fmt tfmt, lrc_stream_t stream);
+
+/*
+ * lrc_distill_grad -- the gradient apart, for a program that has the loss
+ * already: dz_j as above times g, from the lse that lrc_distill gave.
+ *
+ *   lse     device, rows binary32 values
+ *   g       device, rows binary32 upstream gradients of the losses; NULL for
+ *           ones.  A row with g = 0 gets a zero gradient
+ */
+LRC_API lrc_status lrc_distill_grad(const void* Z, const void* T, const int64_t* idx, const float* w, const float* lse,
+                                    const float* g, void* dZ, int64_t rows, int64_t V, int64_t K, int64_t ldz,
+                                    int64_t ldt, int64_t lddz, double tau, lrc_fmt fmt, lrc_fmt tfmt,
+                                    lrc_stream_t stream);
+
 /* Release library-held scratch on every device; the library stays usable. */
 LRC_API lrc_status lrc_shutdown(void);
 

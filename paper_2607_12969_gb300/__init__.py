@@ -17,7 +17,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Sequence, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblrc.so")
@@ -92,6 +92,22 @@ def load() -> ctypes.CDLL:
     L.lrc_probe_peak.restype = i32
     L.lrc_selftest_wait_timeout.argtypes = [i64, vp]
     L.lrc_selftest_wait_timeout.restype = i32
+    L.lrc_q4_row_bytes.argtypes = [i64]
+    L.lrc_q4_row_bytes.restype = i64
+    L.lrc_q4_round.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, i64, i32, vp]
+    L.lrc_q4_round.restype = i32
+    L.lrc_q4_widen.argtypes = [vp, vp, vp, i64, i32, i64, i64, vp, i32, i64, vp]
+    L.lrc_q4_widen.restype = i32
+    L.lrc_q4_apply.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp]
+    L.lrc_q4_apply.restype = i32
+    L.lrc_layer_norm.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, dbl, i32, i32, vp]
+    L.lrc_layer_norm.restype = i32
+    L.lrc_layer_norm_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i32, i32, vp]
+    L.lrc_layer_norm_grad.restype = i32
+    L.lrc_distill.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, dbl, i32, i32, vp]
+    L.lrc_distill.restype = i32
+    L.lrc_distill_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, dbl, i32, i32, vp]
+    L.lrc_distill_grad.restype = i32
     _lib = L
     return L
 
@@ -497,6 +513,130 @@ def lrc_selftest_wait_timeout(limit_ns: int, stream=None) -> None:
 
 
 # --------------------------------------------------------------------------
+# the operators around a compressed layer
+# --------------------------------------------------------------------------
+
+def _check_optional(t, what: str, dtype, elems: int, dev: int, stream) -> None:
+    if t is not None:
+        _check_arg(t, what, dtype, elems, dev, stream)
+
+
+def lrc_q4_row_bytes(n: int) -> int:
+    """Bytes of one row of a 4-bit matrix's codes."""
+    return int(load().lrc_q4_row_bytes(int(n)))
+
+
+def _check_q4(Q, scales, zeros, m, n, group, f, dev, stream) -> None:
+    st, torch = storage_dtype(f), _T()
+    if m > 0 and n > 0 and group > 0:
+        span = ((n + group - 1) // group - 1) * ((m + 15) // 16 * 16) + m
+        _check_arg(Q, "Q", torch.uint8, m * ((n + 127) // 128 * 64), dev, stream)
+        _check_arg(scales, "scales", st, span, dev, stream)
+        _check_optional(zeros, "zeros", torch.uint8, span, dev, stream)
+
+
+def lrc_q4_round(W, wfmt, m: int, n: int, ldw: int, Q, scales, zeros, group: int, fmt, stream=None):
+    """Rounds W to 4-bit codes Q with scales (and zero codes, or None)."""
+    f, fw, dev = _fmt(fmt), _fmt(wfmt), _call_device(stream)
+    _check_arg(W, "W", storage_dtype(fw), _extent(m, n, ldw), dev, stream)
+    _check_q4(Q, scales, zeros, m, n, group, f, dev, stream)
+    _check(load().lrc_q4_round(_ptr(W), fw, m, n, ldw, _ptr(Q), _ptr(scales), _ptr(zeros), group, f, _stream(stream)))
+
+
+def lrc_q4_widen(Q, scales, zeros, group: int, fmt, m: int, n: int, dst, dfmt, ld_dst: int, stream=None):
+    """The values a 4-bit matrix stands for, in format dfmt's storage type."""
+    f, fd, dev = _fmt(fmt), _fmt(dfmt), _call_device(stream)
+    _check_q4(Q, scales, zeros, m, n, group, f, dev, stream)
+    _check_arg(dst, "dst", storage_dtype(fd), _extent(m, n, ld_dst), dev, stream)
+    _check(load().lrc_q4_widen(_ptr(Q), _ptr(scales), _ptr(zeros), group, f, m, n, _ptr(dst), fd, ld_dst,
+                               _stream(stream)))
+
+
+def lrc_q4_apply(Q, scales, zeros, X, A, Y, m: int, n: int, b: int, group: int, fmt, stream=None):
+    """Y = A + X What^T for a 4-bit matrix What and b vectors; A may be None or Y."""
+    f, dev = _fmt(fmt), _call_device(stream)
+    _check_q4(Q, scales, zeros, m, n, group, f, dev, stream)
+    if m > 0 and n > 0 and b > 0:
+        out = output_dtype(f)
+        _check_arg(X, "X", storage_dtype(f), (b - 1) * ((n + 15) // 16 * 16) + n, dev, stream)
+        _check_optional(A, "A", out, b * m, dev, stream)
+        _check_arg(Y, "Y", out, b * m, dev, stream)
+    _check(load().lrc_q4_apply(_ptr(Q), _ptr(scales), _ptr(zeros), _ptr(X), _ptr(A), _ptr(Y), m, n, b, group, f,
+                               _stream(stream)))
+
+
+def lrc_layer_norm(X, gamma, beta, Y, mean, rstd, rows: int, cols: int, ldx: int, ldy: int, eps: float, fmt, pfmt,
+                   stream=None):
+    """Layer norm of the rows of X into Y; gamma, beta, mean and rstd may be None."""
+    f, fp, dev = _fmt(fmt), _fmt(pfmt), _call_device(stream)
+    st, out, pt, f32 = storage_dtype(f), output_dtype(f), storage_dtype(fp), _T().float32
+    if rows > 0 and cols > 0:
+        _check_arg(X, "X", st, (rows - 1) * ldx + cols, dev, stream)
+        _check_optional(gamma, "gamma", pt, cols, dev, stream)
+        _check_optional(beta, "beta", pt, cols, dev, stream)
+        _check_arg(Y, "Y", out, (rows - 1) * ldy + cols, dev, stream)
+        _check_optional(mean, "mean", f32, rows, dev, stream)
+        _check_optional(rstd, "rstd", f32, rows, dev, stream)
+    _check(load().lrc_layer_norm(_ptr(X), _ptr(gamma), _ptr(beta), _ptr(Y), _ptr(mean), _ptr(rstd), rows, cols, ldx, ldy,
+                                 float(eps), f, fp, _stream(stream)))
+
+
+def lrc_layer_norm_grad(dY, X, gamma, mean, rstd, dX, dgamma, dbeta, rows: int, cols: int, lddy: int, ldx: int,
+                        lddx: int, fmt, pfmt, stream=None):
+    """Gradient of lrc_layer_norm; gamma, dX, dgamma and dbeta may be None."""
+    f, fp, dev = _fmt(fmt), _fmt(pfmt), _call_device(stream)
+    st, out, pt, f32 = storage_dtype(f), output_dtype(f), storage_dtype(fp), _T().float32
+    if rows > 0 and cols > 0:
+        _check_arg(dY, "dY", out, (rows - 1) * lddy + cols, dev, stream)
+        _check_arg(X, "X", st, (rows - 1) * ldx + cols, dev, stream)
+        _check_optional(gamma, "gamma", pt, cols, dev, stream)
+        _check_arg(mean, "mean", f32, rows, dev, stream)
+        _check_arg(rstd, "rstd", f32, rows, dev, stream)
+        _check_optional(dX, "dX", st, (rows - 1) * lddx + cols, dev, stream)
+    _check_optional(dgamma, "dgamma", f32, cols, dev, stream)
+    _check_optional(dbeta, "dbeta", f32, cols, dev, stream)
+    _check(load().lrc_layer_norm_grad(_ptr(dY), _ptr(X), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dX), _ptr(dgamma),
+                                      _ptr(dbeta), rows, cols, lddy, ldx, lddx, f, fp, _stream(stream)))
+
+
+def _check_distill(Z, T, idx, w, dZ, rows, V, K, ldz, ldt, lddz, f, ft, dev, stream) -> None:
+    st, tt, torch = storage_dtype(f), storage_dtype(ft), _T()
+    if rows > 0 and V > 0 and K > 0:
+        _check_arg(Z, "Z", st, (rows - 1) * ldz + V, dev, stream)
+        _check_arg(T, "T", tt, (rows - 1) * ldt + K, dev, stream)
+        _check_arg(idx, "idx", torch.int64, (rows - 1) * ldt + K, dev, stream)
+        _check_optional(w, "w", torch.float32, rows, dev, stream)
+        _check_optional(dZ, "dZ", st, (rows - 1) * lddz + V, dev, stream)
+
+
+def lrc_distill(Z, T, idx, w, loss, lse, dZ, rows: int, V: int, K: int, ldz: int, ldt: int, lddz: int, tau: float, fmt,
+                tfmt, stream=None):
+    """Distillation loss of each row of Z against the teacher's top logits T at
+    idx, and its gradient dZ; w, loss, lse and dZ may be None."""
+    f, ft, dev = _fmt(fmt), _fmt(tfmt), _call_device(stream)
+    f32 = _T().float32
+    _check_distill(Z, T, idx, w, dZ, rows, V, K, ldz, ldt, lddz, f, ft, dev, stream)
+    _check_optional(loss, "loss", f32, rows, dev, stream)
+    _check_optional(lse, "lse", f32, rows, dev, stream)
+    _check(load().lrc_distill(_ptr(Z), _ptr(T), _ptr(idx), _ptr(w), _ptr(loss), _ptr(lse), _ptr(dZ), rows, V, K, ldz,
+                              ldt, lddz, float(tau), f, ft, _stream(stream)))
+
+
+def lrc_distill_grad(Z, T, idx, w, lse, g, dZ, rows: int, V: int, K: int, ldz: int, ldt: int, lddz: int, tau: float, fmt,
+                     tfmt, stream=None):
+    """Gradient of lrc_distill's losses apart, from its lse; w and g may be None."""
+    f, ft, dev = _fmt(fmt), _fmt(tfmt), _call_device(stream)
+    f32 = _T().float32
+    _check_distill(Z, T, idx, w, dZ, rows, V, K, ldz, ldt, lddz, f, ft, dev, stream)
+    if rows > 0:
+        _check_arg(lse, "lse", f32, rows, dev, stream)
+        _check_optional(g, "g", f32, rows, dev, stream)
+        _check_arg(dZ, "dZ", storage_dtype(f), 0, dev, stream)
+    _check(load().lrc_distill_grad(_ptr(Z), _ptr(T), _ptr(idx), _ptr(w), _ptr(lse), _ptr(g), _ptr(dZ), rows, V, K, ldz,
+                                   ldt, lddz, float(tau), f, ft, _stream(stream)))
+
+
+# --------------------------------------------------------------------------
 # convenience helpers built only from the entry points above
 # --------------------------------------------------------------------------
 
@@ -520,3 +660,30 @@ def widen_matrix(src, fmt, cols: int, stream=None):
     dst = torch.empty((rows, lrc_packed_ld(cols)), dtype=torch.float64, device=src.device)
     lrc_widen_factors(src, fmt, rows, cols, ld, dst, dst.shape[1], stream)
     return dst
+
+
+class Q4Matrix(NamedTuple):
+    """A matrix as 4-bit codes (q4_matrix): what lrc_q4_apply and lrc_q4_widen take."""
+    Q: object
+    scales: object
+    zeros: object
+    m: int
+    n: int
+    group: int
+    fmt: str
+
+
+def q4_matrix(W, fmt, group: int = 128, zeros: bool = False, stream=None) -> Q4Matrix:
+    """Round a 2-D CUDA tensor into a new 4-bit matrix (lrc_q4_round) whose
+    products take vectors of format fmt."""
+    import torch
+    wfmt = {torch.float64: "f64", torch.float32: "f32", torch.float16: "f16", torch.bfloat16: "bf16"}[W.dtype]
+    m, n = W.shape
+    if W.stride(1) != 1 or (m > 1 and W.stride(0) < n):
+        W = W.contiguous()
+    groups, ldm = (n + group - 1) // group, lrc_packed_ld(m)
+    Q = torch.empty((m, lrc_q4_row_bytes(n)), dtype=torch.uint8, device=W.device)
+    scales = torch.zeros((groups, ldm), dtype=storage_dtype(fmt), device=W.device)
+    z = torch.zeros((groups, ldm), dtype=torch.uint8, device=W.device) if zeros else None
+    lrc_q4_round(W, wfmt, m, n, W.stride(0) if m > 1 else n, Q, scales, z, group, fmt, stream)
+    return Q4Matrix(Q, scales, z, m, n, group, fmt)

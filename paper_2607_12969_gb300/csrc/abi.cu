@@ -499,6 +499,204 @@ lrc_status lrc_probe_peak(int kind, int64_t iters, double* flops_out, lrc_stream
     return run_probe_peak(kind, iters, flops_out, as_stream(stream));
 }
 
+// ---- the operators around a compressed layer ------------------------------
+
+}  // extern "C"
+
+namespace {
+
+bool aligned_to(const void* p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes == 0; }
+
+lrc_status misaligned_element(const char* name) {
+    set_error("%s is not aligned to its element size", name);
+    return LRC_ERR_ALIGNMENT;
+}
+
+lrc_status unsupported(const char* what) {
+    set_error("%s", what);
+    return LRC_ERR_UNSUPPORTED;
+}
+
+// rows x ld elements of up to 8 bytes do not overflow.
+bool extent_ok(int64_t rows, int64_t ld) {
+    int64_t t;
+    return mul_ok(rows, ld, &t) && mul_ok(t, 8, &t);
+}
+
+int64_t out_bytes(lrc_fmt f) { return f == LRC_F16 ? 4 : storage_bytes(f); }
+
+// What the three calls on a 4-bit matrix check of it.
+lrc_status check_q4(const void* Q, const void* scales, const uint8_t* zeros, int64_t m, int64_t n, int64_t group,
+                    int fmt) {
+    if (!valid_fmt(fmt)) return invalid("unknown format %d", fmt);
+    if (fmt == LRC_F64) return unsupported("4-bit matrices have no LRC_F64 scales");
+    if (m <= 0 || n <= 0) return invalid("sizes must be positive (m=%lld n=%lld)", (long long)m, (long long)n);
+    if (group <= 0) return invalid("group = %lld must be positive", (long long)group);
+    if (group != 32 && group != 64 && group != 128) return unsupported("group must be 32, 64 or 128");
+    if (m > INT64_MAX / 2 || n > INT64_MAX / 2 || !extent_ok(lrc_packed_ld(m), (n + 31) / 32) ||
+        !extent_ok(m, lrc_packed_ld(n)))
+        return invalid("size overflow");
+    if (!Q || !scales) return invalid("null pointer");
+    if (!aligned16(Q)) return misaligned("Q");
+    if (!aligned16(scales)) return misaligned("scales");
+    if (!aligned16(zeros)) return misaligned("zeros");
+    return LRC_OK;
+}
+
+// Formats of layer norm's data and parameters.
+lrc_status check_norm(int64_t rows, int64_t cols, int fmt, int pfmt) {
+    if (!valid_fmt(fmt) || !valid_fmt(pfmt)) return invalid("unknown format %d / %d", fmt, pfmt);
+    if (fmt == LRC_F64 || pfmt == LRC_F64) return unsupported("layer norm has no LRC_F64");
+    const lrc_fmt f = plain_fmt((lrc_fmt)fmt), p = plain_fmt((lrc_fmt)pfmt);
+    if (p != LRC_F32 && ((p == LRC_BF16) != (f == LRC_BF16) || f == LRC_F32))
+        return invalid("parameters are binary32 or of X's storage type (formats %d / %d)", fmt, pfmt);
+    if (rows < 0 || cols <= 0) return invalid("bad sizes (rows=%lld cols=%lld)", (long long)rows, (long long)cols);
+    if (rows > 0x7fffffff) return invalid("rows = %lld: at most 2^31 - 1", (long long)rows);
+    return LRC_OK;
+}
+
+lrc_status check_distill(const void* Z, const void* T, const int64_t* idx, const float* w, const void* dZ, int64_t rows,
+                         int64_t V, int64_t K, int64_t ldz, int64_t ldt, int64_t lddz, double tau, int fmt, int tfmt) {
+    if (!valid_fmt(fmt) || !valid_fmt(tfmt)) return invalid("unknown format %d / %d", fmt, tfmt);
+    if (fmt == LRC_F64 || tfmt == LRC_F64) return unsupported("distillation has no LRC_F64");
+    if (rows < 0 || V <= 0 || K <= 0)
+        return invalid("bad sizes (rows=%lld V=%lld K=%lld)", (long long)rows, (long long)V, (long long)K);
+    if (rows > 0x7fffffff) return invalid("rows = %lld: at most 2^31 - 1", (long long)rows);
+    if (ldz < V || ldt < K || (dZ && lddz < V)) return invalid("row pitch below the row's length");
+    if (!extent_ok(rows, ldz) || !extent_ok(rows, ldt) || (dZ && !extent_ok(rows, lddz))) return invalid("size overflow");
+    const float t = (float)tau;
+    if (!(t > 0.f) || isinf(t)) return invalid("tau = %g must be positive and finite in binary32", tau);
+    if (isinf(1.f / t)) return invalid("tau = %g is too small", tau);
+    if (K > distill_max_top()) return unsupported("more than 1024 teacher entries a row");
+    if (rows == 0) return LRC_OK;
+    if (!Z || !T || !idx) return invalid("null pointer");
+    if (!aligned_to(Z, storage_bytes((lrc_fmt)fmt))) return misaligned_element("Z");
+    if (!aligned_to(T, storage_bytes((lrc_fmt)tfmt))) return misaligned_element("T");
+    if (!aligned_to(idx, 8)) return misaligned_element("idx");
+    if (!aligned_to(w, 4)) return misaligned_element("w");
+    if (!aligned_to(dZ, storage_bytes((lrc_fmt)fmt))) return misaligned_element("dZ");
+    return LRC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t lrc_q4_row_bytes(int64_t n) {
+    if (n < 0 || n > INT64_MAX - 127) return -1;
+    return (n + 127) / 128 * 64;
+}
+
+lrc_status lrc_q4_round(const void* W, lrc_fmt wfmt, int64_t m, int64_t n, int64_t ldw, void* Q, void* scales,
+                        uint8_t* zeros, int64_t group, lrc_fmt fmt, lrc_stream_t stream) {
+    lrc_status st = check_q4(Q, scales, zeros, m, n, group, fmt);
+    if (st != LRC_OK) return st;
+    if (!valid_fmt(wfmt)) return invalid("unknown format %d", (int)wfmt);
+    if (ldw < n) return invalid("leading dimension below n");
+    if (!extent_ok(m, ldw)) return invalid("size overflow");
+    if (!W) return invalid("null pointer");
+    if (!aligned_to(W, storage_bytes(wfmt))) return misaligned_element("W");
+    return launch_q4_round(W, plain_fmt(wfmt), m, n, ldw, Q, scales, zeros, (int)group, plain_fmt(fmt),
+                           as_stream(stream));
+}
+
+lrc_status lrc_q4_widen(const void* Q, const void* scales, const uint8_t* zeros, int64_t group, lrc_fmt fmt, int64_t m,
+                        int64_t n, void* dst, lrc_fmt dfmt, int64_t ld_dst, lrc_stream_t stream) {
+    lrc_status st = check_q4(Q, scales, zeros, m, n, group, fmt);
+    if (st != LRC_OK) return st;
+    if (!valid_fmt(dfmt)) return invalid("unknown format %d", (int)dfmt);
+    if (ld_dst < n) return invalid("leading dimension below n");
+    if (!extent_ok(m, ld_dst)) return invalid("size overflow");
+    if (!dst) return invalid("null pointer");
+    if (!aligned_to(dst, storage_bytes(dfmt))) return misaligned_element("dst");
+    return launch_q4_widen(Q, scales, zeros, (int)group, plain_fmt(fmt), m, n, dst, plain_fmt(dfmt), ld_dst,
+                           as_stream(stream));
+}
+
+lrc_status lrc_q4_apply(const void* Q, const void* scales, const uint8_t* zeros, const void* X, const void* A, void* Y,
+                        int64_t m, int64_t n, int64_t b, int64_t group, lrc_fmt fmt, lrc_stream_t stream) {
+    lrc_status st = check_q4(Q, scales, zeros, m, n, group, fmt);
+    if (st != LRC_OK) return st;
+    if (b < 0) return invalid("b = %lld is negative", (long long)b);
+    if (!extent_ok(b, lrc_packed_ld(n)) || !extent_ok(b, m)) return invalid("size overflow");
+    if (b == 0) return LRC_OK;
+    if (!X || !Y) return invalid("null pointer");
+    if (!aligned16(X)) return misaligned("X");
+    if (!aligned16(A)) return misaligned("A");
+    if (!aligned16(Y)) return misaligned("Y");
+    return launch_q4_apply(Q, scales, zeros, X, A, Y, m, n, b, (int)group, plain_fmt(fmt), as_stream(stream));
+}
+
+lrc_status lrc_layer_norm(const void* X, const void* gamma, const void* beta, void* Y, float* mean, float* rstd,
+                          int64_t rows, int64_t cols, int64_t ldx, int64_t ldy, double eps, lrc_fmt fmt, lrc_fmt pfmt,
+                          lrc_stream_t stream) {
+    lrc_status st = check_norm(rows, cols, fmt, pfmt);
+    if (st != LRC_OK) return st;
+    if (ldx < cols || ldy < cols) return invalid("row pitch below cols");
+    if (!extent_ok(rows, ldx) || !extent_ok(rows, ldy)) return invalid("size overflow");
+    if (!(eps >= 0.0) || isinf((float)eps)) return invalid("eps = %g must be finite and not negative", eps);
+    if (rows == 0) return LRC_OK;
+    if (!X || !Y) return invalid("null pointer");
+    const int64_t es = storage_bytes(fmt), ps = storage_bytes(pfmt);
+    if (!aligned_to(X, es)) return misaligned_element("X");
+    if (!aligned_to(Y, out_bytes(fmt))) return misaligned_element("Y");
+    if (!aligned_to(gamma, ps)) return misaligned_element("gamma");
+    if (!aligned_to(beta, ps)) return misaligned_element("beta");
+    if (!aligned_to(mean, 4)) return misaligned_element("mean");
+    if (!aligned_to(rstd, 4)) return misaligned_element("rstd");
+    return launch_layer_norm(X, gamma, beta, Y, mean, rstd, rows, cols, ldx, ldy, (float)eps, plain_fmt(fmt),
+                             plain_fmt(pfmt), as_stream(stream));
+}
+
+lrc_status lrc_layer_norm_grad(const void* dY, const void* X, const void* gamma, const float* mean, const float* rstd,
+                               void* dX, float* dgamma, float* dbeta, int64_t rows, int64_t cols, int64_t lddy,
+                               int64_t ldx, int64_t lddx, lrc_fmt fmt, lrc_fmt pfmt, lrc_stream_t stream) {
+    lrc_status st = check_norm(rows, cols, fmt, pfmt);
+    if (st != LRC_OK) return st;
+    if (lddy < cols || ldx < cols || (dX && lddx < cols)) return invalid("row pitch below cols");
+    if (!extent_ok(rows, lddy) || !extent_ok(rows, ldx) || (dX && !extent_ok(rows, lddx)) || !extent_ok(cols, 512))
+        return invalid("size overflow");
+    if (rows > 0) {
+        if (!dY || !X || !mean || !rstd) return invalid("null pointer");
+        const int64_t es = storage_bytes(fmt);
+        if (!aligned_to(dY, out_bytes(fmt))) return misaligned_element("dY");
+        if (!aligned_to(X, es)) return misaligned_element("X");
+        if (!aligned_to(gamma, storage_bytes(pfmt))) return misaligned_element("gamma");
+        if (!aligned_to(mean, 4)) return misaligned_element("mean");
+        if (!aligned_to(rstd, 4)) return misaligned_element("rstd");
+        if (!aligned_to(dX, es)) return misaligned_element("dX");
+    }
+    if (!aligned_to(dgamma, 4)) return misaligned_element("dgamma");
+    if (!aligned_to(dbeta, 4)) return misaligned_element("dbeta");
+    return launch_layer_norm_grad(dY, X, gamma, mean, rstd, dX, dgamma, dbeta, rows, cols, lddy, ldx, lddx,
+                                  plain_fmt(fmt), plain_fmt(pfmt), as_stream(stream));
+}
+
+lrc_status lrc_distill(const void* Z, const void* T, const int64_t* idx, const float* w, float* loss, float* lse,
+                       void* dZ, int64_t rows, int64_t V, int64_t K, int64_t ldz, int64_t ldt, int64_t lddz, double tau,
+                       lrc_fmt fmt, lrc_fmt tfmt, lrc_stream_t stream) {
+    lrc_status st = check_distill(Z, T, idx, w, dZ, rows, V, K, ldz, ldt, lddz, tau, fmt, tfmt);
+    if (st != LRC_OK) return st;
+    if (rows == 0 || (!loss && !lse && !dZ)) return LRC_OK;
+    if (!aligned_to(loss, 4)) return misaligned_element("loss");
+    if (!aligned_to(lse, 4)) return misaligned_element("lse");
+    return launch_distill(Z, T, idx, w, nullptr, nullptr, loss, lse, dZ, rows, V, K, ldz, ldt, lddz, (float)tau,
+                          plain_fmt(fmt), plain_fmt(tfmt), as_stream(stream));
+}
+
+lrc_status lrc_distill_grad(const void* Z, const void* T, const int64_t* idx, const float* w, const float* lse,
+                            const float* g, void* dZ, int64_t rows, int64_t V, int64_t K, int64_t ldz, int64_t ldt,
+                            int64_t lddz, double tau, lrc_fmt fmt, lrc_fmt tfmt, lrc_stream_t stream) {
+    if (lddz < V) return invalid("row pitch below the row's length");
+    lrc_status st = check_distill(Z, T, idx, w, dZ, rows, V, K, ldz, ldt, lddz, tau, fmt, tfmt);
+    if (st != LRC_OK || rows == 0) return st;
+    if (!lse || !dZ) return invalid("null pointer");
+    if (!aligned_to(lse, 4)) return misaligned_element("lse");
+    if (!aligned_to(g, 4)) return misaligned_element("g");
+    return launch_distill(Z, T, idx, w, lse, g, nullptr, nullptr, dZ, rows, V, K, ldz, ldt, lddz, (float)tau,
+                          plain_fmt(fmt), plain_fmt(tfmt), as_stream(stream));
+}
+
 lrc_status lrc_shutdown(void) {
     release_scratch();
     release_workspaces();

@@ -261,6 +261,29 @@ lrc_status run_tt_svd(const double* T, const TTShape& sh, double* const* cores, 
                       double* spectra_out, cudaStream_t s);
 lrc_status run_tt_left_orthogonalize(const TTShape& sh, double* const* cores, cudaStream_t s);
 
+// 4-bit matrices (q4.cu); fmt and wfmt are plain formats, group 32, 64 or 128
+lrc_status launch_q4_round(const void* W, lrc_fmt wfmt, int64_t m, int64_t n, int64_t ldw, void* Q, void* scales,
+                           uint8_t* zeros, int group, lrc_fmt fmt, cudaStream_t s);
+lrc_status launch_q4_widen(const void* Q, const void* scales, const uint8_t* zeros, int group, lrc_fmt fmt, int64_t m,
+                           int64_t n, void* dst, lrc_fmt dfmt, int64_t ld, cudaStream_t s);
+lrc_status launch_q4_apply(const void* Q, const void* scales, const uint8_t* zeros, const void* X, const void* A, void* Y,
+                           int64_t m, int64_t n, int64_t b, int group, lrc_fmt fmt, cudaStream_t s);
+
+// Layer norm (layer_norm.cu); at most 2^31 - 1 rows
+lrc_status launch_layer_norm(const void* X, const void* gamma, const void* beta, void* Y, float* mean, float* rstd,
+                             int64_t rows, int64_t cols, int64_t ldx, int64_t ldy, float eps, lrc_fmt fmt, lrc_fmt pfmt,
+                             cudaStream_t s);
+lrc_status launch_layer_norm_grad(const void* dY, const void* X, const void* gamma, const float* mean, const float* rstd,
+                                  void* dX, float* dgamma, float* dbeta, int64_t rows, int64_t cols, int64_t lddy,
+                                  int64_t ldx, int64_t lddx, lrc_fmt fmt, lrc_fmt pfmt, cudaStream_t s);
+
+// Distillation (distill.cu); at most 2^31 - 1 rows, distill_max_top() teacher
+// entries a row.  With lse_in the log-sum-exp is taken from there.
+int distill_max_top();
+lrc_status launch_distill(const void* Z, const void* T, const int64_t* idx, const float* w, const float* lse_in,
+                          const float* g, float* loss, float* lse_out, void* dZ, int64_t rows, int64_t V, int64_t K,
+                          int64_t ldz, int64_t ldt, int64_t lddz, float tau, lrc_fmt fmt, lrc_fmt tfmt, cudaStream_t s);
+
 // Measured rate of one arithmetic unit (peak_probe.cu); synchronises s.
 lrc_status run_probe_peak(int kind, int64_t iters, double* flops_out, cudaStream_t s);
 

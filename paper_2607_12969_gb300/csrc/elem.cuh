@@ -1,0 +1,44 @@
+// elem.cuh -- elements of the storage formats as binary32 values, for kernels
+// whose arithmetic is binary32: scalar and 16-byte loads and stores, one
+// rounding to nearest even on the way out.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+namespace lrc {
+namespace el {
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// Sum (or maximum) over the 32 lanes of a warp, in every lane.
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+    return x;
+}
+
+// Element i of an array whose type is known at run time: 0 = binary32,
+// 1 = binary16, 2 = bfloat16.
+__device__ __forceinline__ float load_as(const void* p, int kind, int64_t i) {
+    if (kind == 0) return __ldg(static_cast<const float*>(p) + i);
+    const uint32_t h = __ldg(static_cast<const unsigned short*>(p) + i);
+    if (kind == 1) return __half2float(__ushort_as_half((unsigned short)h));
+    return __uint_as_float(h << 16);
+}
+
+}  // namespace el
+}  // namespace lrc
