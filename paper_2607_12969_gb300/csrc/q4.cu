@@ -6,6 +6,7 @@
 // 64-byte blocks of 128 columns, column 32 j + 8 t + e in word 4 t + j.
 #include "common.cuh"
 #include "elem.cuh"
+#include "tc.cuh"
 
 namespace lrc {
 namespace {
@@ -99,44 +100,216 @@ q4_widen_kernel(const uint32_t* __restrict__ Q, const S* __restrict__ scales, co
     dst[row * ld + c] = wide<D>(el::to_f32(scales[g]), q);
 }
 
-// Product: one warp a row of the matrix and four vectors, one word (8 columns)
-// a lane at a time.
-constexpr int kVectors = 4;
-template <typename X, typename Y>
-__global__ void __launch_bounds__(256)
-q4_apply_kernel(const uint32_t* __restrict__ Q, const X* __restrict__ scales, const uint8_t* __restrict__ zeros,
-                const X* __restrict__ x, const Y* A, Y* y, int64_t m, int64_t n, int64_t b, int group, int64_t blocks,
-                int64_t ldm, int64_t ldn) {
-    const int64_t row = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-    const int lane = threadIdx.x & 31;
-    if (row >= m) return;
-    const int64_t b0 = (int64_t)blockIdx.y * kVectors;
-    float acc[kVectors] = {};
-    for (int64_t w = lane; w < blocks * 16; w += 32) {
-        const int slot = (int)w & 15;
-        const int64_t c0 = (w >> 4) * 128 + ((slot & 3) * 4 + (slot >> 2)) * 8;
-        if (c0 >= n) continue;
-        const uint32_t word = Q[row * blocks * 16 + w];
-        const int64_t g = (c0 / group) * ldm + row;
-        const float s = el::to_f32(scales[g]);
-        const int z = zeros ? zeros[g] : 8;
-        float part[kVectors] = {};
-        for (int e = 0; e < 8 && c0 + e < n; ++e) {
-            const float q = (float)((int)((word >> nibble_shift(e)) & 15u) - z);
+// ---- product ---------------------------------------------------------------
+//
+// Y^T = s (q - z) X^T on the matrix instructions m16n8k16: the integers q - z
+// are exact in binary16 and bfloat16 (1024 + q, or 128 + q, is the code's bits
+// under a constant; subtracting 1024 + z is exact), the matrix is the A operand
+// (16 rows), the vectors are the 8 columns of B.  A warp takes blocks of 128
+// columns: thread (g, t) of the warp (lane 4 g + t) loads 16 bytes of the rows g
+// and g + 8 of a tile, the words 4 t + j, and word j holds its columns of step j,
+// 32 columns or two instructions; the order of columns within an instruction is
+// free as long as B has the same, so the thread's x are 16 consecutive bytes.
+// A group's sum is scaled in binary32 and added to the running one.
+//
+// The warps of a block share 16 MT rows and take every WARPS-th block of
+// columns; their sums are added in shared memory in the order of the warps.
+
+struct Half2 {
+    using type = __half;
+    static constexpr uint32_t kMagic = 0x64006400u;      // 1024 + q
+    static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) {
+        uint32_t d;
+        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+        return d;
+    }
+    static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                               uint32_t b0, uint32_t b1) {
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    }
+};
+struct Bf2 {
+    using type = bf16;
+    static constexpr uint32_t kMagic = 0x43004300u;      // 128 + q
+    static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) {
+        uint32_t d;
+        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+        return d;
+    }
+    static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                               uint32_t b0, uint32_t b1) {
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    }
+};
+
+struct ApplyArgs {
+    const uint4* Q;          // m rows of 4 blocks uint4
+    const void* scales;
+    const uint8_t* zeros;
+    const void* x;           // cols rows of 16-bit elements, pitch ldx
+    const void* A;
+    void* y;
+    int64_t m, n, blocks, ldm, ldx;
+    int cols;                // rows of x: vectors, or three parts of each
+    int64_t vectors;
+    int group;
+};
+
+// 16 bytes of codes, read once.
+__device__ __forceinline__ uint4 load_codes(const uint4* p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+template <typename S, int MT>
+struct Stage {
+    uint4 w[MT][2];
+    S s[MT][2];
+    uint32_t z[MT][2];
+};
+
+// OP: the instructions' element type; S: the scales' type; PARTS: columns of B
+// that make one vector (3: a binary32 vector as hi + mid + lo in bfloat16).
+template <typename OP, typename S, typename Y, int PARTS, int NT, int MT, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32)
+q4_apply_kernel(const ApplyArgs a) {
+    constexpr int kRows = 16 * MT, kCols = 8 * NT;
+    __shared__ float sums[WARPS][kCols][kRows + 1];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int64_t row0 = (int64_t)blockIdx.x * kRows;
+    const int col0 = blockIdx.y * kCols;
+    tc::pdl_wait();
+    tc::pdl_trigger();
+
+    const S* scales = static_cast<const S*>(a.scales);
+    const uint4* q[MT][2];
+    int64_t srow[MT][2];
 #pragma unroll
-            for (int v = 0; v < kVectors; ++v)
-                if (b0 + v < b) part[v] = fmaf(q, el::to_f32(x[(b0 + v) * ldn + c0 + e]), part[v]);
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            int64_t r = row0 + 16 * i + 8 * h + g;
+            if (r >= a.m) r = a.m - 1;               // read again, not written
+            q[i][h] = a.Q + r * a.blocks * 4 + t;
+            srow[i][h] = r;
         }
+    const uint16_t* x[NT];
 #pragma unroll
-        for (int v = 0; v < kVectors; ++v) acc[v] = fmaf(s, part[v], acc[v]);
+    for (int j = 0; j < NT; ++j) {
+        const int c = col0 + 8 * j + g;
+        x[j] = c < a.cols ? static_cast<const uint16_t*>(a.x) + (int64_t)c * a.ldx + 8 * t : nullptr;
+    }
+    // a quad's thread t holds the scale (and zero code) of step t of a block
+    const int groups_of_block = 128 / a.group;
+    const int my_group = t * groups_of_block >> 2;
+    const int64_t groups = (a.n + a.group - 1) / a.group;
+
+    float acc[MT][NT][4] = {};
+    Stage<S, MT> st[2];
+    auto load = [&](Stage<S, MT>& f, int64_t block) {
+        int64_t gr = block * groups_of_block + my_group;
+        if (gr >= groups) gr = groups - 1;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f.w[i][h] = load_codes(q[i][h] + block * 4);
+                f.s[i][h] = scales[gr * a.ldm + srow[i][h]];
+                f.z[i][h] = a.zeros ? a.zeros[gr * a.ldm + srow[i][h]] : 8u;
+            }
+    };
+    auto compute = [&](const Stage<S, MT>& f, int64_t block) {
+        float part[MT][NT][4] = {};
+        const int64_t c0 = block * 128 + 8 * t;
+        const bool whole = block * 128 + 128 <= a.n;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint4 xv[NT];
+#pragma unroll
+            for (int k = 0; k < NT; ++k) {
+                xv[k] = make_uint4(0, 0, 0, 0);
+                if (x[k] == nullptr) continue;
+                const uint16_t* p = x[k] + block * 128 + 32 * j;
+                if (PARTS > 1 || whole || c0 + 32 * j + 8 <= a.n) {
+                    xv[k] = __ldg(reinterpret_cast<const uint4*>(p));
+                } else {
+                    uint32_t e[4] = {};
+                    for (int u = 0; u < 8; ++u)
+                        if (c0 + 32 * j + u < a.n) e[u >> 1] |= (uint32_t)p[u] << (16 * (u & 1));
+                    xv[k] = make_uint4(e[0], e[1], e[2], e[3]);
+                }
+            }
+            const int from = (lane & ~3) | j;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                uint32_t r[2][4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t w = j == 0 ? f.w[i][h].x : j == 1 ? f.w[i][h].y : j == 2 ? f.w[i][h].z : f.w[i][h].w;
+                    const uint32_t z = a.zeros ? __shfl_sync(0xffffffffu, f.z[i][h], from) : 8u;
+                    const uint32_t less = OP::kMagic + z * 0x10001u;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        r[h][u] = OP::sub(((w >> (4 * u)) & 0x000f000fu) | OP::kMagic, less);
+                }
+#pragma unroll
+                for (int k = 0; k < NT; ++k) {
+                    OP::mma(part[i][k], r[0][0], r[1][0], r[0][1], r[1][1], xv[k].x, xv[k].y);
+                    OP::mma(part[i][k], r[0][2], r[1][2], r[0][3], r[1][3], xv[k].z, xv[k].w);
+                }
+            }
+            if (j == 3 || a.group == 32 || (j == 1 && a.group == 64)) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    float s[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) s[h] = __shfl_sync(0xffffffffu, el::to_f32(f.s[i][h]), from);
+#pragma unroll
+                    for (int k = 0; k < NT; ++k)
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            acc[i][k][u] = fmaf(s[u >> 1], part[i][k][u], acc[i][k][u]);
+                            part[i][k][u] = 0.f;
+                        }
+                }
+            }
+        }
+    };
+    int64_t block = warp;
+    if (block < a.blocks) load(st[0], block);
+    for (; block < a.blocks; block += 2 * WARPS) {
+        const int64_t next = block + WARPS;
+        if (next < a.blocks) load(st[1], next);
+        compute(st[0], block);
+        if (next < a.blocks) {
+            if (next + WARPS < a.blocks) load(st[0], next + WARPS);
+            compute(st[1], next);
+        }
     }
 #pragma unroll
-    for (int v = 0; v < kVectors; ++v) {
-        const float r = el::warp_sum(acc[v]);
-        if (lane == 0 && b0 + v < b) {
-            const int64_t at = (b0 + v) * m + row;
-            y[at] = el::from_f32<Y>(A ? r + el::to_f32(A[at]) : r);
-        }
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int k = 0; k < NT; ++k)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                sums[warp][8 * k + 2 * t + (u & 1)][16 * i + 8 * (u >> 1) + g] = acc[i][k][u];
+    __syncthreads();
+    const int used = a.cols - col0 < kCols ? a.cols - col0 : kCols;
+    for (int e = threadIdx.x; e < used / PARTS * kRows; e += WARPS * 32) {
+        const int v = e / kRows, r = e % kRows;
+        if (row0 + r >= a.m) continue;
+        float sum = 0.f;
+#pragma unroll
+        for (int p = PARTS - 1; p >= 0; --p)          // the smallest part first
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) sum += sums[w][v * PARTS + p][r];
+        const int64_t at = (int64_t)(col0 / PARTS + v) * a.m + row0 + r;
+        if (a.A) sum += el::to_f32(static_cast<const Y*>(a.A)[at]);
+        static_cast<Y*>(a.y)[at] = el::from_f32<Y>(sum);
     }
 }
 
@@ -173,19 +346,91 @@ lrc_status widen_as(const void* Q, const void* scales, const uint8_t* zeros, int
     return after_launch("q4_widen_kernel");
 }
 
-template <typename X, typename Y>
+// binary32 vectors as three bfloat16 parts, x = hi + mid + lo exactly (each cut
+// off, not rounded, so that none overflows): rows 3 v, 3 v + 1, 3 v + 2 of
+// `blocks` whole blocks of columns, zeros from n on.  An infinity or NaN is in
+// the first part alone.
+__global__ void __launch_bounds__(256)
+q4_parts_kernel(const float* __restrict__ x, int64_t n, int64_t ldn, int64_t ldp, uint16_t* __restrict__ parts) {
+    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    tc::pdl_wait();
+    tc::pdl_trigger();
+    if (c >= ldp) return;
+    const float v = c < n ? x[(int64_t)blockIdx.y * ldn + c] : 0.f;
+    const uint32_t hi = __float_as_uint(v) & 0xffff0000u;
+    const bool odd = !(fabsf(v) <= 3.402823466e38f);
+    const float rest = odd ? 0.f : v - __uint_as_float(hi);
+    const uint32_t mid = __float_as_uint(rest) & 0xffff0000u;
+    const float last = rest - __uint_as_float(mid);
+    uint16_t* p = parts + (int64_t)blockIdx.y * 3 * ldp + c;
+    p[0] = odd && v != v ? 0x7fffu : (uint16_t)(hi >> 16);
+    p[ldp] = (uint16_t)(mid >> 16);
+    p[2 * ldp] = (uint16_t)(__float_as_uint(last) >> 16);
+}
+
+template <typename OP, typename S, typename Y, int PARTS, int NT, int MT, int WARPS>
+lrc_status apply_launch(const ApplyArgs& a, cudaStream_t s) {
+    unsigned grid;
+    lrc_status st = grid_of(a.m, 16 * MT, "lrc_q4_apply", &grid);
+    if (st != LRC_OK) return st;
+    constexpr int kCols = 8 * NT;
+    static_assert(kCols % PARTS == 0, "whole vectors a tile");
+    const cudaError_t e = launch_pdl(q4_apply_kernel<OP, S, Y, PARTS, NT, MT, WARPS>,
+                                     dim3(grid, (unsigned)((a.cols + kCols - 1) / kCols)), dim3(WARPS * 32), 0, s, a);
+    if (e != cudaSuccess) return cuda_fail(e, "q4_apply_kernel");
+    return after_launch("q4_apply_kernel");
+}
+
+template <typename OP, typename S, typename Y, int PARTS>
+lrc_status apply_tiles(const ApplyArgs& a, cudaStream_t s) {
+    if constexpr (PARTS == 1) {
+        if (a.cols <= 8) return apply_launch<OP, S, Y, 1, 1, 1, 8>(a, s);
+        if (a.cols <= 16) return apply_launch<OP, S, Y, 1, 2, 1, 8>(a, s);
+        if (a.cols <= 32) return apply_launch<OP, S, Y, 1, 4, 1, 8>(a, s);
+        return apply_launch<OP, S, Y, 1, 8, 1, 8>(a, s);
+    } else {
+        return apply_launch<OP, S, Y, 3, 3, 1, 8>(a, s);
+    }
+}
+
+template <typename OP, typename S, typename Y, int PARTS>
 lrc_status apply_as(const void* Q, const void* scales, const uint8_t* zeros, const void* x, const void* A, void* y,
                     int64_t m, int64_t n, int64_t b, int group, cudaStream_t s) {
-    unsigned grid;
-    lrc_status st = grid_of(m * 32, 256, "lrc_q4_apply", &grid);
-    if (st != LRC_OK) return st;
-    for (int64_t b0 = 0; b0 < b; b0 += 65535 * kVectors) {
-        const int64_t nb = b - b0 < 65535 * kVectors ? b - b0 : 65535 * kVectors;
-        const int64_t ldn = lrc_packed_ld(n);
-        q4_apply_kernel<X, Y><<<dim3(grid, (unsigned)((nb + kVectors - 1) / kVectors)), 256, 0, s>>>(
-            (const uint32_t*)Q, (const X*)scales, zeros, (const X*)x + b0 * ldn, A ? (const Y*)A + b0 * m : nullptr,
-            (Y*)y + b0 * m, m, n, nb, group, (n + 127) / 128, lrc_packed_ld(m), ldn);
-        if ((st = after_launch("q4_apply_kernel")) != LRC_OK) return st;
+    ApplyArgs a{};
+    a.Q = (const uint4*)Q;
+    a.scales = scales;
+    a.zeros = zeros;
+    a.m = m;
+    a.n = n;
+    a.blocks = (n + 127) / 128;
+    a.ldm = lrc_packed_ld(m);
+    a.group = group;
+    const int64_t ldn = lrc_packed_ld(n);
+    // at most this many vectors a launch
+    constexpr int64_t kMost = 16384;
+    for (int64_t b0 = 0; b0 < b; b0 += kMost) {
+        const int64_t nb = b - b0 < kMost ? b - b0 : kMost;
+        a.A = A ? (const Y*)A + b0 * m : nullptr;
+        a.y = (Y*)y + b0 * m;
+        a.cols = (int)nb * PARTS;
+        if (PARTS == 1) {
+            a.x = (const uint16_t*)x + b0 * ldn;
+            a.ldx = ldn;
+        } else {
+            a.ldx = a.blocks * 128;
+            void* ws = nullptr;
+            lrc_status st = stream_workspace(s, (size_t)nb * 3 * a.ldx * 2, &ws);
+            if (st != LRC_OK) return st;
+            a.x = ws;
+            unsigned grid;
+            if ((st = grid_of(a.ldx, 256, "lrc_q4_apply", &grid)) != LRC_OK) return st;
+            const cudaError_t e = launch_pdl(q4_parts_kernel, dim3(grid, (unsigned)nb), dim3(256), 0, s,
+                                             (const float*)x + b0 * ldn, n, ldn, a.ldx, (uint16_t*)ws);
+            if (e != cudaSuccess) return cuda_fail(e, "q4_parts_kernel");
+            if ((st = after_launch("q4_parts_kernel")) != LRC_OK) return st;
+        }
+        const lrc_status st = apply_tiles<OP, S, Y, PARTS>(a, s);
+        if (st != LRC_OK) return st;
     }
     return LRC_OK;
 }
@@ -224,10 +469,10 @@ lrc_status launch_q4_widen(const void* Q, const void* scales, const uint8_t* zer
 
 lrc_status launch_q4_apply(const void* Q, const void* scales, const uint8_t* zeros, const void* X, const void* A, void* Y,
                            int64_t m, int64_t n, int64_t b, int group, lrc_fmt fmt, cudaStream_t s) {
-    if (fmt == LRC_F32) return apply_as<float, float>(Q, scales, zeros, X, A, Y, m, n, b, group, s);
-    if (fmt == LRC_BF16) return apply_as<bf16, bf16>(Q, scales, zeros, X, A, Y, m, n, b, group, s);
-    if (fmt == LRC_F16) return apply_as<__half, float>(Q, scales, zeros, X, A, Y, m, n, b, group, s);
-    return apply_as<__half, __half>(Q, scales, zeros, X, A, Y, m, n, b, group, s);
+    if (fmt == LRC_F32) return apply_as<Bf2, float, float, 3>(Q, scales, zeros, X, A, Y, m, n, b, group, s);
+    if (fmt == LRC_BF16) return apply_as<Bf2, bf16, bf16, 1>(Q, scales, zeros, X, A, Y, m, n, b, group, s);
+    if (fmt == LRC_F16) return apply_as<Half2, __half, float, 1>(Q, scales, zeros, X, A, Y, m, n, b, group, s);
+    return apply_as<Half2, __half, __half, 1>(Q, scales, zeros, X, A, Y, m, n, b, group, s);
 }
 
 }  // namespace lrc
