@@ -117,11 +117,21 @@ q4_widen_kernel(const uint32_t* __restrict__ Q, const S* __restrict__ scales, co
 
 struct Half2 {
     using type = __half;
-    static constexpr uint32_t kMagic = 0x64006400u;      // 1024 + q
-    static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) {
-        uint32_t d;
-        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-        return d;
+    // The eight q - z of a word, in order.  1024 + q for the codes in the low four
+    // bits of a byte; 1024 + 16 q for the others, brought to q - z by one exact
+    // multiply-add instead of a shift (shifts and masks share a pipe of half the
+    // multiply-adds' rate, which is what the kernel would wait for).
+    static __device__ __forceinline__ void unpack(uint32_t w, uint32_t z, uint32_t (&r)[4]) {
+        const uint32_t one = 0x64006400u + z * 0x10001u;       // 1024 + z
+        const uint32_t sixteenth = 0x2c002c00u;                // 1 / 16
+        const uint32_t less = 0xd400d400u + z * 0x00100010u;   // -(64 + z)
+        const uint32_t w8 = w >> 8;
+        const uint32_t lo0 = (w & 0x000f000fu) | 0x64006400u, hi0 = (w & 0x00f000f0u) | 0x64006400u;
+        const uint32_t lo1 = (w8 & 0x000f000fu) | 0x64006400u, hi1 = (w8 & 0x00f000f0u) | 0x64006400u;
+        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r[0]) : "r"(lo0), "r"(one));
+        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r[1]) : "r"(hi0), "r"(sixteenth), "r"(less));
+        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r[2]) : "r"(lo1), "r"(one));
+        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r[3]) : "r"(hi1), "r"(sixteenth), "r"(less));
     }
     static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                                uint32_t b0, uint32_t b1) {
@@ -131,11 +141,14 @@ struct Half2 {
 };
 struct Bf2 {
     using type = bf16;
-    static constexpr uint32_t kMagic = 0x43004300u;      // 128 + q
-    static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) {
-        uint32_t d;
-        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-        return d;
+    // 128 + q has no room for a code above the low four bits: a shift for each.
+    static __device__ __forceinline__ void unpack(uint32_t w, uint32_t z, uint32_t (&r)[4]) {
+        const uint32_t less = 0x43004300u + z * 0x10001u;      // 128 + z
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t a = ((w >> (4 * u)) & 0x000f000fu) | 0x43004300u;
+            asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r[u]) : "r"(a), "r"(less));
+        }
     }
     static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                                uint32_t b0, uint32_t b1) {
@@ -151,10 +164,9 @@ struct ApplyArgs {
     const void* x;           // cols rows of 16-bit elements, pitch ldx
     const void* A;
     void* y;
-    int64_t m, n, blocks, ldm, ldx;
+    int64_t m, n, blocks, groups, ldm, ldx;
     int cols;                // rows of x: vectors, or three parts of each
-    int64_t vectors;
-    int group;
+    bool wide;               // A and y are binary32
 };
 
 // 16 bytes of codes, read once.
@@ -165,84 +177,90 @@ __device__ __forceinline__ uint4 load_codes(const uint4* p) {
     return v;
 }
 
+struct Whole { static constexpr bool value = false; };
+struct Ragged { static constexpr bool value = true; };
+
 template <typename S, int MT>
 struct Stage {
     uint4 w[MT][2];
     S s[MT][2];
-    uint32_t z[MT][2];
+    uint8_t z[MT][2];
 };
 
 // OP: the instructions' element type; S: the scales' type; PARTS: columns of B
 // that make one vector (3: a binary32 vector as hi + mid + lo in bfloat16).
-template <typename OP, typename S, typename Y, int PARTS, int NT, int MT, int WARPS>
+template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NT, int MT, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32)
 q4_apply_kernel(const ApplyArgs a) {
-    constexpr int kRows = 16 * MT, kCols = 8 * NT;
+    constexpr int kRows = 16 * MT, kCols = 8 * NT, kGroups = 128 / GROUP;      // groups of a block
     __shared__ float sums[WARPS][kCols][kRows + 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int64_t row0 = (int64_t)blockIdx.x * kRows;
     const int col0 = blockIdx.y * kCols;
-    tc::pdl_wait();
-    tc::pdl_trigger();
 
-    const S* scales = static_cast<const S*>(a.scales);
+    // Rows and columns beyond the last are read again and not written.
     const uint4* q[MT][2];
-    int64_t srow[MT][2];
+    const S* sp[MT][2];
+    const uint8_t* zp[MT][2];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             int64_t r = row0 + 16 * i + 8 * h + g;
-            if (r >= a.m) r = a.m - 1;               // read again, not written
-            q[i][h] = a.Q + r * a.blocks * 4 + t;
-            srow[i][h] = r;
+            if (r >= a.m) r = a.m - 1;
+            q[i][h] = a.Q + (r * a.blocks + warp) * 4 + t;
+            // thread t of a quad holds the scale (and zero code) of step t of a block
+            const int64_t at = (int64_t)(warp * kGroups + t * kGroups / 4) * a.ldm + r;
+            sp[i][h] = static_cast<const S*>(a.scales) + at;
+            zp[i][h] = ZEROS ? a.zeros + at : nullptr;
         }
     const uint16_t* x[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        const int c = col0 + 8 * j + g;
-        x[j] = c < a.cols ? static_cast<const uint16_t*>(a.x) + (int64_t)c * a.ldx + 8 * t : nullptr;
+        const int c = min(col0 + 8 * j + g, a.cols - 1);
+        x[j] = static_cast<const uint16_t*>(a.x) + (int64_t)c * a.ldx + warp * 128 + 8 * t;
     }
-    // a quad's thread t holds the scale (and zero code) of step t of a block
-    const int groups_of_block = 128 / a.group;
-    const int my_group = t * groups_of_block >> 2;
-    const int64_t groups = (a.n + a.group - 1) / a.group;
+    tc::pdl_wait();
+    tc::pdl_trigger();
 
     float acc[MT][NT][4] = {};
     Stage<S, MT> st[2];
+    // Loads block `block` and moves the pointers on.  Steps of a ragged last block
+    // whose group does not exist take another scale: their x are zeros.
     auto load = [&](Stage<S, MT>& f, int64_t block) {
-        int64_t gr = block * groups_of_block + my_group;
-        if (gr >= groups) gr = groups - 1;
+        const bool there = GROUP == 128 || block * kGroups + t * kGroups / 4 < a.groups;
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                f.w[i][h] = load_codes(q[i][h] + block * 4);
-                f.s[i][h] = scales[gr * a.ldm + srow[i][h]];
-                f.z[i][h] = a.zeros ? a.zeros[gr * a.ldm + srow[i][h]] : 8u;
+                f.w[i][h] = load_codes(q[i][h]);
+                f.s[i][h] = there ? __ldg(sp[i][h]) : el::from_f32<S>(0.f);
+                if (ZEROS) f.z[i][h] = there ? __ldg(zp[i][h]) : 0;
+                q[i][h] += WARPS * 4;
+                sp[i][h] += (int64_t)WARPS * kGroups * a.ldm;
+                if (ZEROS) zp[i][h] += (int64_t)WARPS * kGroups * a.ldm;
             }
     };
-    auto compute = [&](const Stage<S, MT>& f, int64_t block) {
-        float part[MT][NT][4] = {};
-        const int64_t c0 = block * 128 + 8 * t;
-        const bool whole = block * 128 + 128 <= a.n;
+    // left: columns of the block from the thread's first one on
+    auto compute = [&](const Stage<S, MT>& f, auto ragged, int left) {
+        float part[MT][NT][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             uint4 xv[NT];
 #pragma unroll
             for (int k = 0; k < NT; ++k) {
-                xv[k] = make_uint4(0, 0, 0, 0);
-                if (x[k] == nullptr) continue;
-                const uint16_t* p = x[k] + block * 128 + 32 * j;
-                if (PARTS > 1 || whole || c0 + 32 * j + 8 <= a.n) {
+                const uint16_t* p = x[k] + 32 * j;
+                if (!decltype(ragged)::value || 32 * j + 8 <= left) {
                     xv[k] = __ldg(reinterpret_cast<const uint4*>(p));
                 } else {
                     uint32_t e[4] = {};
+#pragma unroll
                     for (int u = 0; u < 8; ++u)
-                        if (c0 + 32 * j + u < a.n) e[u >> 1] |= (uint32_t)p[u] << (16 * (u & 1));
+                        if (32 * j + u < left) e[u >> 1] |= (uint32_t)p[u] << (16 * (u & 1));
                     xv[k] = make_uint4(e[0], e[1], e[2], e[3]);
                 }
             }
+            constexpr int kSteps = GROUP / 32;           // steps of a group
             const int from = (lane & ~3) | j;
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
@@ -250,45 +268,51 @@ q4_apply_kernel(const ApplyArgs a) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const uint32_t w = j == 0 ? f.w[i][h].x : j == 1 ? f.w[i][h].y : j == 2 ? f.w[i][h].z : f.w[i][h].w;
-                    const uint32_t z = a.zeros ? __shfl_sync(0xffffffffu, f.z[i][h], from) : 8u;
-                    const uint32_t less = OP::kMagic + z * 0x10001u;
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        r[h][u] = OP::sub(((w >> (4 * u)) & 0x000f000fu) | OP::kMagic, less);
+                    uint32_t z = 8;
+                    if (ZEROS) z = GROUP == 128 ? f.z[i][h] : __shfl_sync(0xffffffffu, f.z[i][h], from);
+                    OP::unpack(w, z, r[h]);
                 }
 #pragma unroll
                 for (int k = 0; k < NT; ++k) {
+                    if (j % kSteps == 0) part[i][k][0] = part[i][k][1] = part[i][k][2] = part[i][k][3] = 0.f;
                     OP::mma(part[i][k], r[0][0], r[1][0], r[0][1], r[1][1], xv[k].x, xv[k].y);
                     OP::mma(part[i][k], r[0][2], r[1][2], r[0][3], r[1][3], xv[k].z, xv[k].w);
                 }
-            }
-            if (j == 3 || a.group == 32 || (j == 1 && a.group == 64)) {
+                if ((j + 1) % kSteps == 0) {
 #pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    float s[2];
+                    for (int h = 0; h < 2; ++h) {
+                        float s = el::to_f32(f.s[i][h]);
+                        if (GROUP != 128) s = __shfl_sync(0xffffffffu, s, from);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) s[h] = __shfl_sync(0xffffffffu, el::to_f32(f.s[i][h]), from);
-#pragma unroll
-                    for (int k = 0; k < NT; ++k)
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            acc[i][k][u] = fmaf(s[u >> 1], part[i][k][u], acc[i][k][u]);
-                            part[i][k][u] = 0.f;
+                        for (int k = 0; k < NT; ++k) {
+                            acc[i][k][2 * h] = fmaf(s, part[i][k][2 * h], acc[i][k][2 * h]);
+                            acc[i][k][2 * h + 1] = fmaf(s, part[i][k][2 * h + 1], acc[i][k][2 * h + 1]);
                         }
+                    }
                 }
             }
         }
+#pragma unroll
+        for (int k = 0; k < NT; ++k) x[k] += WARPS * 128;
     };
+    // x is padded with zeros where it is made of parts
+    const int64_t whole = PARTS > 1 ? a.blocks : a.n / 128;
     int64_t block = warp;
     if (block < a.blocks) load(st[0], block);
-    for (; block < a.blocks; block += 2 * WARPS) {
-        const int64_t next = block + WARPS;
-        if (next < a.blocks) load(st[1], next);
-        compute(st[0], block);
-        if (next < a.blocks) {
-            if (next + WARPS < a.blocks) load(st[0], next + WARPS);
-            compute(st[1], next);
-        }
+    while (block + WARPS < whole) {
+        load(st[1], block + WARPS);
+        compute(st[0], Whole(), 0);
+        if (block + 2 * WARPS < a.blocks) load(st[0], block + 2 * WARPS);
+        compute(st[1], Whole(), 0);
+        block += 2 * WARPS;
+    }
+    // at most two blocks are left, the last of them perhaps ragged
+    if (block < a.blocks) {
+        const bool more = block + WARPS < a.blocks;
+        if (more) load(st[1], block + WARPS);
+        if (block < whole) compute(st[0], Whole(), 0);
+        else compute(st[0], Ragged(), (int)(a.n - block * 128) - 8 * t);
+        if (more) compute(st[1], Ragged(), (int)(a.n - (block + WARPS) * 128) - 8 * t);
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -298,7 +322,7 @@ q4_apply_kernel(const ApplyArgs a) {
             for (int u = 0; u < 4; ++u)
                 sums[warp][8 * k + 2 * t + (u & 1)][16 * i + 8 * (u >> 1) + g] = acc[i][k][u];
     __syncthreads();
-    const int used = a.cols - col0 < kCols ? a.cols - col0 : kCols;
+    const int used = min(a.cols - col0, kCols);
     for (int e = threadIdx.x; e < used / PARTS * kRows; e += WARPS * 32) {
         const int v = e / kRows, r = e % kRows;
         if (row0 + r >= a.m) continue;
@@ -308,8 +332,14 @@ q4_apply_kernel(const ApplyArgs a) {
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) sum += sums[w][v * PARTS + p][r];
         const int64_t at = (int64_t)(col0 / PARTS + v) * a.m + row0 + r;
-        if (a.A) sum += el::to_f32(static_cast<const Y*>(a.A)[at]);
-        static_cast<Y*>(a.y)[at] = el::from_f32<Y>(sum);
+        if (PARTS > 1 || a.wide) {
+            if (a.A) sum += static_cast<const float*>(a.A)[at];
+            static_cast<float*>(a.y)[at] = sum;
+        } else {
+            using T = typename OP::type;
+            if (a.A) sum += el::to_f32(static_cast<const T*>(a.A)[at]);
+            static_cast<T*>(a.y)[at] = el::from_f32<T>(sum);
+        }
     }
 }
 
@@ -368,28 +398,38 @@ q4_parts_kernel(const float* __restrict__ x, int64_t n, int64_t ldn, int64_t ldp
     p[2 * ldp] = (uint16_t)(__float_as_uint(last) >> 16);
 }
 
-template <typename OP, typename S, typename Y, int PARTS, int NT, int MT, int WARPS>
-lrc_status apply_launch(const ApplyArgs& a, cudaStream_t s) {
+template <typename OP, typename S, int PARTS, int NT, int MT, int WARPS>
+lrc_status apply_launch(const ApplyArgs& a, int group, cudaStream_t s) {
     unsigned grid;
     lrc_status st = grid_of(a.m, 16 * MT, "lrc_q4_apply", &grid);
     if (st != LRC_OK) return st;
     constexpr int kCols = 8 * NT;
     static_assert(kCols % PARTS == 0, "whole vectors a tile");
-    const cudaError_t e = launch_pdl(q4_apply_kernel<OP, S, Y, PARTS, NT, MT, WARPS>,
-                                     dim3(grid, (unsigned)((a.cols + kCols - 1) / kCols)), dim3(WARPS * 32), 0, s, a);
-    if (e != cudaSuccess) return cuda_fail(e, "q4_apply_kernel");
-    return after_launch("q4_apply_kernel");
+    auto go = [&](auto kernel) {
+        const cudaError_t e = launch_pdl(kernel, dim3(grid, (unsigned)((a.cols + kCols - 1) / kCols)), dim3(WARPS * 32), 0, s,
+                                         a);
+        if (e != cudaSuccess) return cuda_fail(e, "q4_apply_kernel");
+        return after_launch("q4_apply_kernel");
+    };
+    if (a.zeros) {
+        if (group == 32) return go(q4_apply_kernel<OP, S, PARTS, 32, true, NT, MT, WARPS>);
+        if (group == 64) return go(q4_apply_kernel<OP, S, PARTS, 64, true, NT, MT, WARPS>);
+        return go(q4_apply_kernel<OP, S, PARTS, 128, true, NT, MT, WARPS>);
+    }
+    if (group == 32) return go(q4_apply_kernel<OP, S, PARTS, 32, false, NT, MT, WARPS>);
+    if (group == 64) return go(q4_apply_kernel<OP, S, PARTS, 64, false, NT, MT, WARPS>);
+    return go(q4_apply_kernel<OP, S, PARTS, 128, false, NT, MT, WARPS>);
 }
 
-template <typename OP, typename S, typename Y, int PARTS>
-lrc_status apply_tiles(const ApplyArgs& a, cudaStream_t s) {
+template <typename OP, typename S, int PARTS>
+lrc_status apply_tiles(const ApplyArgs& a, int group, cudaStream_t s) {
     if constexpr (PARTS == 1) {
-        if (a.cols <= 8) return apply_launch<OP, S, Y, 1, 1, 1, 8>(a, s);
-        if (a.cols <= 16) return apply_launch<OP, S, Y, 1, 2, 1, 8>(a, s);
-        if (a.cols <= 32) return apply_launch<OP, S, Y, 1, 4, 1, 8>(a, s);
-        return apply_launch<OP, S, Y, 1, 8, 1, 8>(a, s);
+        if (a.cols <= 8) return apply_launch<OP, S, 1, 1, 1, 8>(a, group, s);
+        if (a.cols <= 16) return apply_launch<OP, S, 1, 2, 1, 8>(a, group, s);
+        if (a.cols <= 32) return apply_launch<OP, S, 1, 4, 1, 8>(a, group, s);
+        return apply_launch<OP, S, 1, 8, 1, 8>(a, group, s);
     } else {
-        return apply_launch<OP, S, Y, 3, 3, 1, 8>(a, s);
+        return apply_launch<OP, S, 3, 3, 1, 8>(a, group, s);
     }
 }
 
@@ -404,7 +444,8 @@ lrc_status apply_as(const void* Q, const void* scales, const uint8_t* zeros, con
     a.n = n;
     a.blocks = (n + 127) / 128;
     a.ldm = lrc_packed_ld(m);
-    a.group = group;
+    a.groups = (n + group - 1) / group;
+    a.wide = sizeof(Y) == 4;
     const int64_t ldn = lrc_packed_ld(n);
     // at most this many vectors a launch
     constexpr int64_t kMost = 16384;
@@ -429,7 +470,7 @@ lrc_status apply_as(const void* Q, const void* scales, const uint8_t* zeros, con
             if (e != cudaSuccess) return cuda_fail(e, "q4_parts_kernel");
             if ((st = after_launch("q4_parts_kernel")) != LRC_OK) return st;
         }
-        const lrc_status st = apply_tiles<OP, S, Y, PARTS>(a, s);
+        const lrc_status st = apply_tiles<OP, S, PARTS>(a, group, s);
         if (st != LRC_OK) return st;
     }
     return LRC_OK;
