@@ -524,6 +524,7 @@ LRC_API lrc_status lrc_probe_peak(int kind, int64_t iters, double* flops_out, lr
  *   zeros   device, the same shape in bytes, or NULL; values 0 ... 15
  *   group   columns that share a scale: 32, 64 or 128, else
  *           LRC_ERR_UNSUPPORTED (LRC_F64 too)
+ *   m, n    at most 2^30, else LRC_ERR_UNSUPPORTED
  *
  * Q, scales and zeros are 16-byte aligned.
  */

@@ -432,14 +432,15 @@ lrc_status lrc_device_status(lrc_stream_t stream) {
     const uint32_t t3 = take_tt3_tc_error();
     const uint32_t tn = take_ttn_tc_error();
     const uint32_t sk = take_skinny_error() | take_split_error() | take_split32_error();
+    const uint32_t q4 = take_q4_error();
     const uint32_t t = t1 | t3 | tn;
-    if (a == 0xffffffffu || t1 == 0xffffffffu || t3 == 0xffffffffu || tn == 0xffffffffu || sk == 0xffffffffu) {
+    if (q4 == 0xffffffffu || a == 0xffffffffu || t1 == 0xffffffffu || t3 == 0xffffffffu || tn == 0xffffffffu || sk == 0xffffffffu) {
         set_error("could not read the device error words");
         return LRC_ERR_CUDA;
     }
-    if (a | t | sk) {
-        set_error("a bounded device wait gave up (apply code 0x%x, TT code 0x%x, small-batch apply code 0x%x)", a,
-                  t, sk);
+    if (a | t | sk | q4) {
+        set_error("a bounded device wait gave up (apply code 0x%x, TT code 0x%x, small-batch apply code 0x%x, "
+                  "4-bit product code 0x%x)", a, t, sk, q4);
         return LRC_ERR_TIMEOUT;
     }
     return LRC_OK;
@@ -536,6 +537,7 @@ lrc_status check_q4(const void* Q, const void* scales, const uint8_t* zeros, int
     if (m > INT64_MAX / 2 || n > INT64_MAX / 2 || !extent_ok(lrc_packed_ld(m), (n + 31) / 32) ||
         !extent_ok(m, lrc_packed_ld(n)))
         return invalid("size overflow");
+    if (m > 1 << 30 || n > 1 << 30) return unsupported("a 4-bit matrix has at most 2^30 rows and columns");
     if (!Q || !scales) return invalid("null pointer");
     if (!aligned16(Q)) return misaligned("Q");
     if (!aligned16(scales)) return misaligned("scales");

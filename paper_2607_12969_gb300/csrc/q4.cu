@@ -112,8 +112,11 @@ q4_widen_kernel(const uint32_t* __restrict__ Q, const S* __restrict__ scales, co
 // free as long as B has the same, so the thread's x are 16 consecutive bytes.
 // A group's sum is scaled in binary32 and added to the running one.
 //
-// The warps of a block share 16 MT rows and take every WARPS-th block of
-// columns; their sums are added in shared memory in the order of the warps.
+// A block has WARPS warps of 16 MT rows each.  One more warp brings codes, x,
+// scales and zero codes of two blocks of columns at a time by TMA into a ring of
+// stages that all warps read, so that x passes the L2 port once a block and not
+// once a warp.  The blocks of a cluster share the columns of a tile; their sums
+// are added in the order of their ranks through distributed shared memory.
 
 struct Half2 {
     using type = __half;
@@ -164,183 +167,208 @@ struct ApplyArgs {
     const void* x;           // cols rows of 16-bit elements, pitch ldx
     const void* A;
     void* y;
-    int64_t m, n, blocks, groups, ldm, ldx;
-    int cols;                // rows of x: vectors, or three parts of each
+    int64_t m, blocks, groups, ldm, ldx, xcols;
+    int cols, xrows;         // rows of x (vectors, or three parts of each), and of its boxes
+    int split;               // blocks of a cluster, which share the columns of a tile
     bool wide;               // A and y are binary32
 };
 
-// 16 bytes of codes, read once.
-__device__ __forceinline__ uint4 load_codes(const uint4* p) {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+__device__ unsigned int g_err_q4;
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The float at the same place of the shared memory of block `rank` of the cluster.
+__device__ __forceinline__ float cluster_load(const float* p, uint32_t rank) {
+    uint32_t at;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
     return v;
 }
 
-struct Whole { static constexpr bool value = false; };
-struct Ragged { static constexpr bool value = true; };
-
-template <typename S, int MT>
-struct Stage {
-    uint4 w[MT][2];
-    S s[MT][2];
-    uint8_t z[MT][2];
+// Shared memory of a stage, two blocks of columns (256): rows of 128 bytes of
+// codes, four boxes of 64 columns of x (kCols rows of 128 bytes), both with the
+// 128-byte swizzle; scales and zero codes of the two blocks' groups, kRows a group.
+template <typename S, int GROUP, bool ZEROS, int NT, int MT, int WARPS>
+struct StageOf {
+    static constexpr int kRows = 16 * MT * WARPS, kCols = 8 * NT, kGroups = 256 / GROUP;
+    static constexpr int kX = kRows * 128, kXBox = kCols * 128, kScales = kX + 4 * kXBox;
+    static constexpr int kScaleBytes = kGroups * kRows * (int)sizeof(S), kZeroBytes = ZEROS ? kGroups * kRows : 0;
+    static constexpr int kZeros = kScales + (kScaleBytes + 127) / 128 * 128;       // TMA boxes start at 128 bytes
+    static constexpr int kPitch = (kZeros + kZeroBytes + 1023) / 1024 * 1024;
+    static constexpr int kSums = kCols * (kRows + 1) * 4;                           // after the last stage
 };
 
 // OP: the instructions' element type; S: the scales' type; PARTS: columns of B
-// that make one vector (3: a binary32 vector as hi + mid + lo in bfloat16).
-template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NT, int MT, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32)
-q4_apply_kernel(const ApplyArgs a) {
-    constexpr int kRows = 16 * MT, kCols = 8 * NT, kGroups = 128 / GROUP;      // groups of a block
-    __shared__ float sums[WARPS][kCols][kRows + 1];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int64_t row0 = (int64_t)blockIdx.x * kRows;
+// that make one vector (3: a binary32 vector as hi + mid + lo in bfloat16);
+// DEPTH: stages of the ring.
+template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NT, int MT, int WARPS, int DEPTH, int RESIDENT>
+__global__ void __launch_bounds__(WARPS * 32 + 32, RESIDENT)
+q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap xmap,
+                const __grid_constant__ CUtensorMap smap, const __grid_constant__ CUtensorMap zmap,
+                const __grid_constant__ ApplyArgs a) {
+    using St = StageOf<S, GROUP, ZEROS, NT, MT, WARPS>;
+    constexpr int kRows = St::kRows, kCols = St::kCols, kGroups = 128 / GROUP;      // groups of a block
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t full[DEPTH], empty[DEPTH];
+    __shared__ int abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = blockIdx.x % a.split;
+    const int64_t row0 = (int64_t)(blockIdx.x / a.split) * kRows;
     const int col0 = blockIdx.y * kCols;
-
-    // Rows and columns beyond the last are read again and not written.
-    const uint4* q[MT][2];
-    const S* sp[MT][2];
-    const uint8_t* zp[MT][2];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            int64_t r = row0 + 16 * i + 8 * h + g;
-            if (r >= a.m) r = a.m - 1;
-            q[i][h] = a.Q + (r * a.blocks + warp) * 4 + t;
-            // thread t of a quad holds the scale (and zero code) of step t of a block
-            const int64_t at = (int64_t)(warp * kGroups + t * kGroups / 4) * a.ldm + r;
-            sp[i][h] = static_cast<const S*>(a.scales) + at;
-            zp[i][h] = ZEROS ? a.zeros + at : nullptr;
+    const int pairs = (int)((a.blocks + 1) / 2);
+    const int mine = (pairs - rank + a.split - 1) / a.split;         // stages of this block
+    uint8_t* ring = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
+    volatile int* abort = &abort_flag;
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (int d = 0; d < DEPTH; ++d) {
+            tc::mbar_init(&full[d], 1);
+            tc::mbar_init(&empty[d], WARPS);
         }
-    const uint16_t* x[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int c = min(col0 + 8 * j + g, a.cols - 1);
-        x[j] = static_cast<const uint16_t*>(a.x) + (int64_t)c * a.ldx + warp * 128 + 8 * t;
+        tc::fence_barrier_init();
     }
+    __syncthreads();
     tc::pdl_wait();
     tc::pdl_trigger();
 
+    if (warp == WARPS) {
+        if (lane == 0) {
+            const uint32_t bytes = kRows * 128 + a.xrows * 512 + St::kScaleBytes + St::kZeroBytes;
+            int k = 0;
+            for (; k < mine; ++k) {
+                const int slot = k % DEPTH;
+                if (k >= DEPTH && !tc::mbar_wait(&empty[slot], (k / DEPTH & 1) ^ 1, abort, &g_err_q4, 1u)) break;
+                uint64_t* bar = &full[slot];
+                uint8_t* to = ring + slot * St::kPitch;
+                const int unit = rank + k * a.split;
+                tc::mbar_arrive_expect_tx(bar, bytes);
+                tc::tma_load_2d(to, &qmap, unit * 128, (int32_t)row0, bar);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    tc::tma_load_2d(to + St::kX + q * St::kXBox, &xmap, unit * 256 + q * 64, col0, bar);
+                tc::tma_load_2d(to + St::kScales, &smap, (int32_t)row0, unit * 2 * kGroups, bar);
+                if (ZEROS) tc::tma_load_2d(to + St::kZeros, &zmap, (int32_t)row0, unit * 2 * kGroups, bar);
+            }
+            // no copy is in flight when the block goes on
+            volatile int no_abort = 0;
+            for (int u = k > DEPTH ? k - DEPTH : 0; u < k; ++u)
+                tc::mbar_wait(&full[u % DEPTH], u / DEPTH & 1, &no_abort, &g_err_q4, 1u);
+        }
+        __syncwarp();
+    }
     float acc[MT][NT][4] = {};
-    Stage<S, MT> st[2];
-    // Loads block `block` and moves the pointers on.  Steps of a ragged last block
-    // whose group does not exist take another scale: their x are zeros.
-    auto load = [&](Stage<S, MT>& f, int64_t block) {
-        const bool there = GROUP == 128 || block * kGroups + t * kGroups / 4 < a.groups;
+    const int g = lane >> 2, t = lane & 3;
+    // Row of eight (and column of eight) that the lanes of g take: neighbouring g
+    // in opposite halves of a swizzled row, so that 16-byte loads meet no bank
+    // conflict.
+    const int rho = g >> 1 | (g & 1) << 2;
+    if (warp < WARPS) {
+        const int swz[2] = {(t ^ rho) << 4, ((4 | t) ^ rho) << 4};
+        const int at = (16 * MT * warp + rho) * 128, sat = 16 * MT * warp + rho;
+        int xat[NT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int k = 0; k < NT; ++k)      // columns beyond the last read the last again (a broadcast)
+            xat[k] = min(8 * k + rho, a.xrows - 1);
+        int slot = 0;
+        uint32_t phase = 0;
+        for (int k = 0; k < mine; ++k) {
+            if (!tc::mbar_wait(&full[slot], phase, abort, &g_err_q4, 1u)) break;
+            const uint8_t* from = ring + slot * St::kPitch;
+            const int halves = 2 * (rank + k * a.split) + 1 < a.blocks ? 2 : 1;
+#pragma unroll 1
+            for (int half = 0; half < halves; ++half) {
+                uint4 w[MT][2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                f.w[i][h] = load_codes(q[i][h]);
-                f.s[i][h] = there ? __ldg(sp[i][h]) : el::from_f32<S>(0.f);
-                if (ZEROS) f.z[i][h] = there ? __ldg(zp[i][h]) : 0;
-                q[i][h] += WARPS * 4;
-                sp[i][h] += (int64_t)WARPS * kGroups * a.ldm;
-                if (ZEROS) zp[i][h] += (int64_t)WARPS * kGroups * a.ldm;
-            }
-    };
-    // left: columns of the block from the thread's first one on
-    auto compute = [&](const Stage<S, MT>& f, auto ragged, int left) {
-        float part[MT][NT][4];
+                for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint4 xv[NT];
+                    for (int h = 0; h < 2; ++h)
+                        w[i][h] = *reinterpret_cast<const uint4*>(from + at + (2 * i + h) * 1024 + (half ? swz[1] : swz[0]));
+                const S* scales = reinterpret_cast<const S*>(from + St::kScales) + half * kGroups * kRows + sat;
+                const uint8_t* zeros = from + St::kZeros + half * kGroups * kRows + sat;
+                const uint8_t* xs = from + St::kX + half * 2 * St::kXBox;
+                float part[MT][NT][4];
 #pragma unroll
-            for (int k = 0; k < NT; ++k) {
-                const uint16_t* p = x[k] + 32 * j;
-                if (!decltype(ragged)::value || 32 * j + 8 <= left) {
-                    xv[k] = __ldg(reinterpret_cast<const uint4*>(p));
-                } else {
-                    uint32_t e[4] = {};
+                for (int j = 0; j < 4; ++j) {
+                    uint4 xv[NT];
 #pragma unroll
-                    for (int u = 0; u < 8; ++u)
-                        if (32 * j + u < left) e[u >> 1] |= (uint32_t)p[u] << (16 * (u & 1));
-                    xv[k] = make_uint4(e[0], e[1], e[2], e[3]);
-                }
-            }
-            constexpr int kSteps = GROUP / 32;           // steps of a group
-            const int from = (lane & ~3) | j;
+                    for (int c = 0; c < NT; ++c)
+                        xv[c] = *reinterpret_cast<const uint4*>(xs + (j >> 1) * St::kXBox + xat[c] * 128 +
+                                                                (((4 * (j & 1) + t) ^ (xat[c] & 7)) << 4));
+                    constexpr int kSteps = GROUP / 32;           // steps of a group
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                uint32_t r[2][4];
+                    for (int i = 0; i < MT; ++i) {
+                        uint32_t r[2][4];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t w = j == 0 ? f.w[i][h].x : j == 1 ? f.w[i][h].y : j == 2 ? f.w[i][h].z : f.w[i][h].w;
-                    uint32_t z = 8;
-                    if (ZEROS) z = GROUP == 128 ? f.z[i][h] : __shfl_sync(0xffffffffu, f.z[i][h], from);
-                    OP::unpack(w, z, r[h]);
-                }
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t word = j == 0 ? w[i][h].x : j == 1 ? w[i][h].y : j == 2 ? w[i][h].z : w[i][h].w;
+                            OP::unpack(word, ZEROS ? zeros[j / kSteps * kRows + 16 * i + 8 * h] : 8u, r[h]);
+                        }
 #pragma unroll
-                for (int k = 0; k < NT; ++k) {
-                    if (j % kSteps == 0) part[i][k][0] = part[i][k][1] = part[i][k][2] = part[i][k][3] = 0.f;
-                    OP::mma(part[i][k], r[0][0], r[1][0], r[0][1], r[1][1], xv[k].x, xv[k].y);
-                    OP::mma(part[i][k], r[0][2], r[1][2], r[0][3], r[1][3], xv[k].z, xv[k].w);
-                }
-                if ((j + 1) % kSteps == 0) {
+                        for (int c = 0; c < NT; ++c) {
+                            if (j % kSteps == 0) part[i][c][0] = part[i][c][1] = part[i][c][2] = part[i][c][3] = 0.f;
+                            OP::mma(part[i][c], r[0][0], r[1][0], r[0][1], r[1][1], xv[c].x, xv[c].y);
+                            OP::mma(part[i][c], r[0][2], r[1][2], r[0][3], r[1][3], xv[c].z, xv[c].w);
+                        }
+                        if ((j + 1) % kSteps == 0) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float s = el::to_f32(f.s[i][h]);
-                        if (GROUP != 128) s = __shfl_sync(0xffffffffu, s, from);
+                            for (int h = 0; h < 2; ++h) {
+                                const float s = el::to_f32(scales[j / kSteps * kRows + 16 * i + 8 * h]);
 #pragma unroll
-                        for (int k = 0; k < NT; ++k) {
-                            acc[i][k][2 * h] = fmaf(s, part[i][k][2 * h], acc[i][k][2 * h]);
-                            acc[i][k][2 * h + 1] = fmaf(s, part[i][k][2 * h + 1], acc[i][k][2 * h + 1]);
+                                for (int c = 0; c < NT; ++c) {
+                                    acc[i][c][2 * h] = fmaf(s, part[i][c][2 * h], acc[i][c][2 * h]);
+                                    acc[i][c][2 * h + 1] = fmaf(s, part[i][c][2 * h + 1], acc[i][c][2 * h + 1]);
+                                }
+                            }
                         }
                     }
                 }
             }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&empty[slot]);
+            if (++slot == DEPTH) {
+                slot = 0;
+                phase ^= 1;
+            }
         }
-#pragma unroll
-        for (int k = 0; k < NT; ++k) x[k] += WARPS * 128;
-    };
-    // x is padded with zeros where it is made of parts
-    const int64_t whole = PARTS > 1 ? a.blocks : a.n / 128;
-    int64_t block = warp;
-    if (block < a.blocks) load(st[0], block);
-    while (block + WARPS < whole) {
-        load(st[1], block + WARPS);
-        compute(st[0], Whole(), 0);
-        if (block + 2 * WARPS < a.blocks) load(st[0], block + 2 * WARPS);
-        compute(st[1], Whole(), 0);
-        block += 2 * WARPS;
     }
-    // at most two blocks are left, the last of them perhaps ragged
-    if (block < a.blocks) {
-        const bool more = block + WARPS < a.blocks;
-        if (more) load(st[1], block + WARPS);
-        if (block < whole) compute(st[0], Whole(), 0);
-        else compute(st[0], Ragged(), (int)(a.n - block * 128) - 8 * t);
-        if (more) compute(st[1], Ragged(), (int)(a.n - (block + WARPS) * 128) - 8 * t);
+    __syncthreads();                                              // the ring is free
+    float(*sums)[kRows + 1] = reinterpret_cast<float(*)[kRows + 1]>(ring);
+    if (warp < WARPS) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+                for (int u = 0; u < 4; ++u)      // column 2 t + u of eight, t or t + 4 of the vectors
+                    sums[8 * c + t + 4 * (u & 1)][16 * (MT * warp + i) + 8 * (u >> 1) + rho] = acc[i][c][u];
     }
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int k = 0; k < NT; ++k)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                sums[warp][8 * k + 2 * t + (u & 1)][16 * i + 8 * (u >> 1) + g] = acc[i][k][u];
-    __syncthreads();
-    const int used = min(a.cols - col0, kCols);
-    for (int e = threadIdx.x; e < used / PARTS * kRows; e += WARPS * 32) {
+    if (a.split > 1) cluster_sync();
+    else __syncthreads();
+    const int used = min(a.cols - col0, kCols) / PARTS;           // vectors of this tile
+    for (int e = rank * (WARPS * 32 + 32) + threadIdx.x; e < used * kRows; e += a.split * (WARPS * 32 + 32)) {
         const int v = e / kRows, r = e % kRows;
         if (row0 + r >= a.m) continue;
         float sum = 0.f;
 #pragma unroll
-        for (int p = PARTS - 1; p >= 0; --p)          // the smallest part first
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) sum += sums[w][v * PARTS + p][r];
-        const int64_t at = (int64_t)(col0 / PARTS + v) * a.m + row0 + r;
+        for (int p = PARTS - 1; p >= 0; --p) {                    // the smallest part first
+            if (a.split > 1)
+                for (int w = 0; w < a.split; ++w) sum += cluster_load(&sums[v * PARTS + p][r], w);
+            else
+                sum += sums[v * PARTS + p][r];
+        }
+        const int64_t o = (int64_t)(col0 / PARTS + v) * a.m + row0 + r;
         if (PARTS > 1 || a.wide) {
-            if (a.A) sum += static_cast<const float*>(a.A)[at];
-            static_cast<float*>(a.y)[at] = sum;
+            if (a.A) sum += static_cast<const float*>(a.A)[o];
+            static_cast<float*>(a.y)[o] = sum;
         } else {
             using T = typename OP::type;
-            if (a.A) sum += el::to_f32(static_cast<const T*>(a.A)[at]);
-            static_cast<T*>(a.y)[at] = el::from_f32<T>(sum);
+            if (a.A) sum += el::to_f32(static_cast<const T*>(a.A)[o]);
+            static_cast<T*>(a.y)[o] = el::from_f32<T>(sum);
         }
     }
+    if (a.split > 1) cluster_sync();                              // the sums stay until they are read
 }
 
 lrc_status grid_of(int64_t threads, int per, const char* what, unsigned* out) {
@@ -398,38 +426,90 @@ q4_parts_kernel(const float* __restrict__ x, int64_t n, int64_t ldn, int64_t ldp
     p[2 * ldp] = (uint16_t)(__float_as_uint(last) >> 16);
 }
 
-template <typename OP, typename S, int PARTS, int NT, int MT, int WARPS>
-lrc_status apply_launch(const ApplyArgs& a, int group, cudaStream_t s) {
-    unsigned grid;
-    lrc_status st = grid_of(a.m, 16 * MT, "lrc_q4_apply", &grid);
-    if (st != LRC_OK) return st;
-    constexpr int kCols = 8 * NT;
+constexpr CUtensorMapDataType map_type(float) { return CU_TENSOR_MAP_DATA_TYPE_FLOAT32; }
+constexpr CUtensorMapDataType map_type(__half) { return CU_TENSOR_MAP_DATA_TYPE_FLOAT16; }
+constexpr CUtensorMapDataType map_type(bf16) { return CU_TENSOR_MAP_DATA_TYPE_BFLOAT16; }
+
+template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NT, int MT, int WARPS, int DEPTH, int RESIDENT>
+lrc_status apply_launch(ApplyArgs a, cudaStream_t s) {
+    using St = StageOf<S, GROUP, ZEROS, NT, MT, WARPS>;
+    constexpr int kCols = St::kCols, kRows = St::kRows;
     static_assert(kCols % PARTS == 0, "whole vectors a tile");
-    auto go = [&](auto kernel) {
-        const cudaError_t e = launch_pdl(kernel, dim3(grid, (unsigned)((a.cols + kCols - 1) / kCols)), dim3(WARPS * 32), 0, s,
-                                         a);
-        if (e != cudaSuccess) return cuda_fail(e, "q4_apply_kernel");
-        return after_launch("q4_apply_kernel");
-    };
-    if (a.zeros) {
-        if (group == 32) return go(q4_apply_kernel<OP, S, PARTS, 32, true, NT, MT, WARPS>);
-        if (group == 64) return go(q4_apply_kernel<OP, S, PARTS, 64, true, NT, MT, WARPS>);
-        return go(q4_apply_kernel<OP, S, PARTS, 128, true, NT, MT, WARPS>);
+    a.xrows = a.cols < kCols ? a.cols : kCols;
+    CUtensorMap qm, xm, sm, zm{};
+    lrc_status st = encode_map_2d(&qm, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.Q, a.blocks * 64, a.m, a.blocks * 64, 128, kRows,
+                                  true, "Q");
+    if (st != LRC_OK) return st;
+    st = encode_map_2d(&xm, map_type(typename OP::type()), a.x, a.xcols, a.cols, a.ldx * 2, 64, (uint32_t)a.xrows, true,
+                       "X");
+    if (st != LRC_OK) return st;
+    st = encode_map_2d(&sm, map_type(S()), a.scales, a.m, a.groups, a.ldm * (int64_t)sizeof(S), kRows, St::kGroups, false,
+                       "scales");
+    if (st != LRC_OK) return st;
+    if (ZEROS) {
+        st = encode_map_2d(&zm, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.zeros, a.m, a.groups, a.ldm, kRows, St::kGroups, false,
+                           "zeros");
+        if (st != LRC_OK) return st;
     }
-    if (group == 32) return go(q4_apply_kernel<OP, S, PARTS, 32, false, NT, MT, WARPS>);
-    if (group == 64) return go(q4_apply_kernel<OP, S, PARTS, 64, false, NT, MT, WARPS>);
-    return go(q4_apply_kernel<OP, S, PARTS, 128, false, NT, MT, WARPS>);
+    // Blocks that share a tile's columns: the number that fills the
+    // multiprocessors' waves best, a wave's fixed part taken as four stages.
+    const int64_t tiles = (a.m + kRows - 1) / kRows, chunks = (a.cols + kCols - 1) / kCols, pairs = (a.blocks + 1) / 2;
+    const int64_t slots = (int64_t)RESIDENT * sm_count();
+    int64_t best = INT64_MAX;
+    for (int split = 1; split <= 8 && split <= pairs; ++split) {
+        const int64_t cost = (tiles * chunks * split + slots - 1) / slots * ((pairs + split - 1) / split + 4);
+        if (cost < best) {
+            best = cost;
+            a.split = split;
+        }
+    }
+    unsigned grid;
+    if ((st = grid_of(tiles * a.split, 1, "lrc_q4_apply", &grid)) != LRC_OK) return st;
+    auto kernel = q4_apply_kernel<OP, S, PARTS, GROUP, ZEROS, NT, MT, WARPS, DEPTH, RESIDENT>;
+    constexpr int kSmem = DEPTH * St::kPitch + 1024;
+    static_assert(St::kSums <= DEPTH * St::kPitch, "the sums lie in the ring");
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return cuda_fail(e, "q4_apply_kernel");
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(grid, (unsigned)chunks);
+    cfg.blockDim = dim3(WARPS * 32 + 32);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)a.split;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.split > 1 ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, kernel, qm, xm, sm, zm, a);
+    if (e != cudaSuccess) return cuda_fail(e, "q4_apply_kernel");
+    return after_launch("q4_apply_kernel");
 }
 
+template <typename OP, typename S, int PARTS, int NT, int MT, int WARPS, int DEPTH, int RESIDENT>
+lrc_status apply_groups(const ApplyArgs& a, int group, cudaStream_t s) {
+    if (a.zeros) {
+        if (group == 32) return apply_launch<OP, S, PARTS, 32, true, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
+        if (group == 64) return apply_launch<OP, S, PARTS, 64, true, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
+        return apply_launch<OP, S, PARTS, 128, true, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
+    }
+    if (group == 32) return apply_launch<OP, S, PARTS, 32, false, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
+    if (group == 64) return apply_launch<OP, S, PARTS, 64, false, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
+    return apply_launch<OP, S, PARTS, 128, false, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
+}
+
+#define Q4V 1, 8, 4, 2
 template <typename OP, typename S, int PARTS>
 lrc_status apply_tiles(const ApplyArgs& a, int group, cudaStream_t s) {
     if constexpr (PARTS == 1) {
-        if (a.cols <= 8) return apply_launch<OP, S, 1, 1, 1, 8>(a, group, s);
-        if (a.cols <= 16) return apply_launch<OP, S, 1, 2, 1, 8>(a, group, s);
-        if (a.cols <= 32) return apply_launch<OP, S, 1, 4, 1, 8>(a, group, s);
-        return apply_launch<OP, S, 1, 8, 1, 8>(a, group, s);
+        if (a.cols <= 8) return apply_groups<OP, S, 1, 1, Q4V>(a, group, s);
+        if (a.cols <= 16) return apply_groups<OP, S, 1, 2, 1, 8, 4, 2>(a, group, s);
+        if (a.cols <= 32) return apply_groups<OP, S, 1, 4, 1, 8, 2, 2>(a, group, s);
+        return apply_groups<OP, S, 1, 8, 1, 8, 3, 1>(a, group, s);
     } else {
-        return apply_launch<OP, S, 3, 3, 1, 8>(a, group, s);
+        return apply_groups<OP, S, 3, 3, 1, 8, 3, 2>(a, group, s);
     }
 }
 
@@ -441,7 +521,6 @@ lrc_status apply_as(const void* Q, const void* scales, const uint8_t* zeros, con
     a.scales = scales;
     a.zeros = zeros;
     a.m = m;
-    a.n = n;
     a.blocks = (n + 127) / 128;
     a.ldm = lrc_packed_ld(m);
     a.groups = (n + group - 1) / group;
@@ -457,8 +536,9 @@ lrc_status apply_as(const void* Q, const void* scales, const uint8_t* zeros, con
         if (PARTS == 1) {
             a.x = (const uint16_t*)x + b0 * ldn;
             a.ldx = ldn;
+            a.xcols = n;
         } else {
-            a.ldx = a.blocks * 128;
+            a.ldx = a.xcols = a.blocks * 128;
             void* ws = nullptr;
             lrc_status st = stream_workspace(s, (size_t)nb * 3 * a.ldx * 2, &ws);
             if (st != LRC_OK) return st;
@@ -514,6 +594,16 @@ lrc_status launch_q4_apply(const void* Q, const void* scales, const uint8_t* zer
     if (fmt == LRC_BF16) return apply_as<Bf2, bf16, bf16, 1>(Q, scales, zeros, X, A, Y, m, n, b, group, s);
     if (fmt == LRC_F16) return apply_as<Half2, __half, float, 1>(Q, scales, zeros, X, A, Y, m, n, b, group, s);
     return apply_as<Half2, __half, __half, 1>(Q, scales, zeros, X, A, Y, m, n, b, group, s);
+}
+
+uint32_t take_q4_error() {
+    unsigned int v = 0;
+    if (cudaMemcpyFromSymbol(&v, g_err_q4, sizeof v) != cudaSuccess) return 0xffffffffu;
+    if (v) {
+        const unsigned int z = 0;
+        cudaMemcpyToSymbol(g_err_q4, &z, sizeof z);
+    }
+    return v;
 }
 
 }  // namespace lrc
