@@ -141,10 +141,19 @@ struct Half2 {
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     }
+    // The same with nothing to add to.
+    static __device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                                     uint32_t b0, uint32_t b1) {
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+    }
 };
 struct Bf2 {
     using type = bf16;
     // 128 + q has no room for a code above the low four bits: a shift for each.
+    // (The upper halves of products with 2^28, 2^24, 2^20 in the place of shifts,
+    // on the multipliers' pipe, are slower: 47 us against 43 for 16384 x 16384.)
     static __device__ __forceinline__ void unpack(uint32_t w, uint32_t z, uint32_t (&r)[4]) {
         const uint32_t less = 0x43004300u + z * 0x10001u;      // 128 + z
 #pragma unroll
@@ -157,6 +166,13 @@ struct Bf2 {
                                                uint32_t b0, uint32_t b1) {
         asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    }
+    // The same with nothing to add to.
+    static __device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                                     uint32_t b0, uint32_t b1) {
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
     }
 };
 
@@ -267,24 +283,24 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     if (warp < WARPS) {
         const int swz[2] = {(t ^ rho) << 4, ((4 | t) ^ rho) << 4};
         const int at = (16 * MT * warp + rho) * 128, sat = 16 * MT * warp + rho;
-        int xat[NT];
-#pragma unroll
-        for (int k = 0; k < NT; ++k)      // columns beyond the last read the last again (a broadcast)
-            xat[k] = min(8 * k + rho, a.xrows - 1);
+        // Columns beyond the last read the last again (a broadcast) where one tile
+        // of eight holds them all; else whatever is there: their sums are not used.
+        const int xrow = NT == 1 ? min(rho, a.xrows - 1) : rho;
+        const int xat[2] = {xrow * 128 + ((t ^ xrow) << 4), xrow * 128 + (((4 | t) ^ xrow) << 4)};
         int slot = 0;
         uint32_t phase = 0;
         for (int k = 0; k < mine; ++k) {
             if (!tc::mbar_wait(&full[slot], phase, abort, &g_err_q4, 1u)) break;
             const uint8_t* from = ring + slot * St::kPitch;
-            const int halves = 2 * (rank + k * a.split) + 1 < a.blocks ? 2 : 1;
-#pragma unroll 1
-            for (int half = 0; half < halves; ++half) {
+            // (a second block beyond the last has x, codes and scales of zero)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
                 uint4 w[MT][2];
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        w[i][h] = *reinterpret_cast<const uint4*>(from + at + (2 * i + h) * 1024 + (half ? swz[1] : swz[0]));
+                        w[i][h] = *reinterpret_cast<const uint4*>(from + at + (2 * i + h) * 1024 + swz[half]);
                 const S* scales = reinterpret_cast<const S*>(from + St::kScales) + half * kGroups * kRows + sat;
                 const uint8_t* zeros = from + St::kZeros + half * kGroups * kRows + sat;
                 const uint8_t* xs = from + St::kX + half * 2 * St::kXBox;
@@ -294,8 +310,7 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                     uint4 xv[NT];
 #pragma unroll
                     for (int c = 0; c < NT; ++c)
-                        xv[c] = *reinterpret_cast<const uint4*>(xs + (j >> 1) * St::kXBox + xat[c] * 128 +
-                                                                (((4 * (j & 1) + t) ^ (xat[c] & 7)) << 4));
+                        xv[c] = *reinterpret_cast<const uint4*>(xs + (j >> 1) * St::kXBox + c * 1024 + xat[j & 1]);
                     constexpr int kSteps = GROUP / 32;           // steps of a group
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
@@ -307,8 +322,8 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                         }
 #pragma unroll
                         for (int c = 0; c < NT; ++c) {
-                            if (j % kSteps == 0) part[i][c][0] = part[i][c][1] = part[i][c][2] = part[i][c][3] = 0.f;
-                            OP::mma(part[i][c], r[0][0], r[1][0], r[0][1], r[1][1], xv[c].x, xv[c].y);
+                            if (j % kSteps == 0) OP::mma_first(part[i][c], r[0][0], r[1][0], r[0][1], r[1][1], xv[c].x, xv[c].y);
+                            else OP::mma(part[i][c], r[0][0], r[1][0], r[0][1], r[1][1], xv[c].x, xv[c].y);
                             OP::mma(part[i][c], r[0][2], r[1][2], r[0][3], r[1][3], xv[c].z, xv[c].w);
                         }
                         if ((j + 1) % kSteps == 0) {
@@ -500,7 +515,7 @@ lrc_status apply_groups(const ApplyArgs& a, int group, cudaStream_t s) {
     return apply_launch<OP, S, PARTS, 128, false, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
 }
 
-#define Q4V 1, 8, 4, 2
+#define Q4V 1, 16, 3, 1
 template <typename OP, typename S, int PARTS>
 lrc_status apply_tiles(const ApplyArgs& a, int group, cudaStream_t s) {
     if constexpr (PARTS == 1) {
