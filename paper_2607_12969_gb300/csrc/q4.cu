@@ -118,6 +118,14 @@ q4_widen_kernel(const uint32_t* __restrict__ Q, const S* __restrict__ scales, co
 // once a warp.  The blocks of a cluster share the columns of a tile; their sums
 // are added in the order of their ranks through distributed shared memory.
 
+// (a & mask) | bits as one instruction.
+template <uint32_t MASK, uint32_t BITS>
+__device__ __forceinline__ uint32_t pick(uint32_t a) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(a), "n"(MASK), "n"(BITS));
+    return d;
+}
+
 struct Half2 {
     using type = __half;
     // The eight q - z of a word, in order.  1024 + q for the codes in the low four
@@ -129,8 +137,8 @@ struct Half2 {
         const uint32_t sixteenth = 0x2c002c00u;                // 1 / 16
         const uint32_t less = 0xd400d400u + z * 0x00100010u;   // -(64 + z)
         const uint32_t w8 = w >> 8;
-        const uint32_t lo0 = (w & 0x000f000fu) | 0x64006400u, hi0 = (w & 0x00f000f0u) | 0x64006400u;
-        const uint32_t lo1 = (w8 & 0x000f000fu) | 0x64006400u, hi1 = (w8 & 0x00f000f0u) | 0x64006400u;
+        const uint32_t lo0 = pick<0x000f000fu, 0x64006400u>(w), hi0 = pick<0x00f000f0u, 0x64006400u>(w);
+        const uint32_t lo1 = pick<0x000f000fu, 0x64006400u>(w8), hi1 = pick<0x00f000f0u, 0x64006400u>(w8);
         asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r[0]) : "r"(lo0), "r"(one));
         asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r[1]) : "r"(hi0), "r"(sixteenth), "r"(less));
         asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r[2]) : "r"(lo1), "r"(one));
@@ -158,7 +166,7 @@ struct Bf2 {
         const uint32_t less = 0x43004300u + z * 0x10001u;      // 128 + z
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const uint32_t a = ((w >> (4 * u)) & 0x000f000fu) | 0x43004300u;
+            const uint32_t a = pick<0x000f000fu, 0x43004300u>(w >> (4 * u));
             asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r[u]) : "r"(a), "r"(less));
         }
     }
