@@ -4,6 +4,10 @@
 //
 // What[i][c] = s (q - z).  The codes' layout is the one include/lrc.h states:
 // 64-byte blocks of 128 columns, column 32 j + 8 t + e in word 4 t + j.
+#include <math.h>
+
+#include <atomic>
+
 #include "common.cuh"
 #include "elem.cuh"
 #include "tc.cuh"
@@ -112,11 +116,15 @@ q4_widen_kernel(const uint32_t* __restrict__ Q, const S* __restrict__ scales, co
 // free as long as B has the same, so the thread's x are 16 consecutive bytes.
 // A group's sum is scaled in binary32 and added to the running one.
 //
-// A block has WARPS warps of 16 MT rows each.  One more warp brings codes, x,
-// scales and zero codes of two blocks of columns at a time by TMA into a ring of
-// stages that all warps read, so that x passes the L2 port once a block and not
-// once a warp.  The blocks of a cluster share the columns of a tile; their sums
-// are added in the order of their ranks through distributed shared memory.
+// A block has R groups of 16 rows and two warps for each, which take alternate
+// pairs of blocks of columns.  One more warp brings codes, x, scales and zero
+// codes of 512 columns at a time by TMA into a ring of stages that all warps
+// read, so that x passes the L2 port once a block and not once a warp.  The
+// blocks of a cluster share the columns of a tile; their sums are added in the
+// order of their ranks through distributed shared memory.
+//
+// What bounds it: the unpacking, 11 (bfloat16) or 9 (binary16) instructions for
+// eight codes, 7 or 5 of them on the pipe of half rate; and HBM.
 
 // (a & mask) | bits as one instruction.
 template <uint32_t MASK, uint32_t BITS>
@@ -193,7 +201,7 @@ struct ApplyArgs {
     void* y;
     int64_t m, blocks, groups, ldm, ldx, xcols;
     int cols, xrows;         // rows of x (vectors, or three parts of each), and of its boxes
-    int split;               // blocks of a cluster, which share the columns of a tile
+    int R, split, depth;     // groups of 16 rows of a tile; blocks of a cluster; stages of the ring
     bool wide;               // A and y are binary32
 };
 
@@ -211,45 +219,56 @@ __device__ __forceinline__ float cluster_load(const float* p, uint32_t rank) {
     return v;
 }
 
-// Shared memory of a stage, two blocks of columns (256): rows of 128 bytes of
-// codes, four boxes of 64 columns of x (kCols rows of 128 bytes), both with the
-// 128-byte swizzle; scales and zero codes of the two blocks' groups, kRows a group.
-template <typename S, int GROUP, bool ZEROS, int NT, int MT, int WARPS>
+// Shared memory of a stage of 512 columns for 16 R rows: two boxes of 128 bytes of
+// codes a row, eight boxes of 64 columns of x (kCols rows of 128 bytes), all with
+// the 128-byte swizzle; scales and zero codes of the groups, 16 R values a group.
+template <typename S, int GROUP, bool ZEROS, int NT>
 struct StageOf {
-    static constexpr int kRows = 16 * MT * WARPS, kCols = 8 * NT, kGroups = 256 / GROUP;
-    static constexpr int kX = kRows * 128, kXBox = kCols * 128, kScales = kX + 4 * kXBox;
-    static constexpr int kScaleBytes = kGroups * kRows * (int)sizeof(S), kZeroBytes = ZEROS ? kGroups * kRows : 0;
-    static constexpr int kZeros = kScales + (kScaleBytes + 127) / 128 * 128;       // TMA boxes start at 128 bytes
-    static constexpr int kPitch = (kZeros + kZeroBytes + 1023) / 1024 * 1024;
-    static constexpr int kSums = kCols * (kRows + 1) * 4;                           // after the last stage
+    static constexpr int kCols = 8 * NT, kGroups = 512 / GROUP, kXBox = kCols * 128;
+    int codes, scales, zeros, scale_bytes, pitch;
+    __host__ __device__ explicit StageOf(int R)
+        : codes(R * 2048), scales(2 * codes + 8 * kXBox), zeros(0), scale_bytes(kGroups * 16 * R * (int)sizeof(S)), pitch(0) {
+        zeros = scales + (scale_bytes + 127) / 128 * 128;                          // TMA boxes start at 128 bytes
+        pitch = (zeros + (ZEROS ? kGroups * 16 * R : 0) + 1023) / 1024 * 1024;
+    }
+    __host__ __device__ int bytes(int R, int xrows) const {                        // what the copies bring
+        return 2 * codes + xrows * 1024 + scale_bytes + (ZEROS ? kGroups * 16 * R : 0);
+    }
 };
 
+// Groups of 16 rows of a tile at most (17 warps of a block have 96 registers a
+// thread, 13 have 128).
+constexpr int most_rows(int NT) { return NT > 2 ? 6 : 8; }
+// Columns of B that a tile uses: whole vectors.
+constexpr int used_cols(int NT, int PARTS) { return 8 * NT / PARTS * PARTS; }
+constexpr int kMostDepth = 8;      // stages of a ring
+
 // OP: the instructions' element type; S: the scales' type; PARTS: columns of B
-// that make one vector (3: a binary32 vector as hi + mid + lo in bfloat16);
-// DEPTH: stages of the ring.
-template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NT, int MT, int WARPS, int DEPTH, int RESIDENT>
-__global__ void __launch_bounds__(WARPS * 32 + 32, RESIDENT)
+// that make one vector (3: a binary32 vector as hi + mid + lo in bfloat16).
+template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NT>
+__global__ void __launch_bounds__(64 * most_rows(NT) + 32, 1)
 q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap xmap,
                 const __grid_constant__ CUtensorMap smap, const __grid_constant__ CUtensorMap zmap,
                 const __grid_constant__ ApplyArgs a) {
-    using St = StageOf<S, GROUP, ZEROS, NT, MT, WARPS>;
-    constexpr int kRows = St::kRows, kCols = St::kCols, kGroups = 128 / GROUP;      // groups of a block
+    using St = StageOf<S, GROUP, ZEROS, NT>;
+    const St lay(a.R);
+    constexpr int kCols = St::kCols;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t full[DEPTH], empty[DEPTH];
+    __shared__ uint64_t full[kMostDepth], empty[kMostDepth];
     __shared__ int abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = blockIdx.x % a.split;
-    const int64_t row0 = (int64_t)(blockIdx.x / a.split) * kRows;
-    const int col0 = blockIdx.y * kCols;
-    const int pairs = (int)((a.blocks + 1) / 2);
-    const int mine = (pairs - rank + a.split - 1) / a.split;         // stages of this block
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = 2 * a.R, threads = 64 * a.R + 32;
+    const int rows = 16 * a.R, rank = blockIdx.x % a.split;
+    const int64_t row0 = (int64_t)(blockIdx.x / a.split) * rows;
+    const int col0 = blockIdx.y * used_cols(NT, PARTS);
+    const int stages = (int)((a.blocks + 3) / 4);
+    const int mine = (stages - rank + a.split - 1) / a.split;         // stages of this block
     uint8_t* ring = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
     volatile int* abort = &abort_flag;
     if (threadIdx.x == 0) {
         abort_flag = 0;
-        for (int d = 0; d < DEPTH; ++d) {
+        for (int d = 0; d < a.depth; ++d) {
             tc::mbar_init(&full[d], 1);
-            tc::mbar_init(&empty[d], WARPS);
+            tc::mbar_init(&empty[d], warps);
         }
         tc::fence_barrier_init();
     }
@@ -257,92 +276,96 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     tc::pdl_wait();
     tc::pdl_trigger();
 
-    if (warp == WARPS) {
+    if (warp == warps) {
         if (lane == 0) {
-            const uint32_t bytes = kRows * 128 + a.xrows * 512 + St::kScaleBytes + St::kZeroBytes;
-            int k = 0;
+            const uint32_t bytes = lay.bytes(a.R, a.xrows);
+            int k = 0, slot = 0;
+            uint32_t phase = 1;
             for (; k < mine; ++k) {
-                const int slot = k % DEPTH;
-                if (k >= DEPTH && !tc::mbar_wait(&empty[slot], (k / DEPTH & 1) ^ 1, abort, &g_err_q4, 1u)) break;
+                if (k >= a.depth && !tc::mbar_wait(&empty[slot], phase, abort, &g_err_q4, 1u)) break;
                 uint64_t* bar = &full[slot];
-                uint8_t* to = ring + slot * St::kPitch;
+                uint8_t* to = ring + slot * lay.pitch;
                 const int unit = rank + k * a.split;
                 tc::mbar_arrive_expect_tx(bar, bytes);
-                tc::tma_load_2d(to, &qmap, unit * 128, (int32_t)row0, bar);
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    tc::tma_load_2d(to + St::kX + q * St::kXBox, &xmap, unit * 256 + q * 64, col0, bar);
-                tc::tma_load_2d(to + St::kScales, &smap, (int32_t)row0, unit * 2 * kGroups, bar);
-                if (ZEROS) tc::tma_load_2d(to + St::kZeros, &zmap, (int32_t)row0, unit * 2 * kGroups, bar);
+                for (int q = 0; q < 2; ++q)
+                    tc::tma_load_2d(to + q * lay.codes, &qmap, unit * 256 + q * 128, (int32_t)row0, bar);
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    tc::tma_load_2d(to + 2 * lay.codes + q * St::kXBox, &xmap, unit * 512 + q * 64, col0, bar);
+                tc::tma_load_2d(to + lay.scales, &smap, (int32_t)row0, unit * St::kGroups, bar);
+                if (ZEROS) tc::tma_load_2d(to + lay.zeros, &zmap, (int32_t)row0, unit * St::kGroups, bar);
+                if (++slot == a.depth) {
+                    slot = 0;
+                    phase ^= 1;
+                }
             }
             // no copy is in flight when the block goes on
             volatile int no_abort = 0;
-            for (int u = k > DEPTH ? k - DEPTH : 0; u < k; ++u)
-                tc::mbar_wait(&full[u % DEPTH], u / DEPTH & 1, &no_abort, &g_err_q4, 1u);
+            for (int u = k > a.depth ? k - a.depth : 0; u < k; ++u)
+                tc::mbar_wait(&full[u % a.depth], u / a.depth & 1, &no_abort, &g_err_q4, 1u);
         }
         __syncwarp();
     }
-    float acc[MT][NT][4] = {};
-    const int g = lane >> 2, t = lane & 3;
+    float acc[NT][4] = {};
+    const int g = lane >> 2, t = lane & 3, half = warp & 1;
     // Row of eight (and column of eight) that the lanes of g take: neighbouring g
     // in opposite halves of a swizzled row, so that 16-byte loads meet no bank
     // conflict.
     const int rho = g >> 1 | (g & 1) << 2;
-    if (warp < WARPS) {
+    const int row = 16 * (warp >> 1) + rho;           // and row + 8
+    if (warp < warps) {
         const int swz[2] = {(t ^ rho) << 4, ((4 | t) ^ rho) << 4};
-        const int at = (16 * MT * warp + rho) * 128, sat = 16 * MT * warp + rho;
         // Columns beyond the last read the last again (a broadcast) where one tile
         // of eight holds them all; else whatever is there: their sums are not used.
         const int xrow = NT == 1 ? min(rho, a.xrows - 1) : rho;
         const int xat[2] = {xrow * 128 + ((t ^ xrow) << 4), xrow * 128 + (((4 | t) ^ xrow) << 4)};
-        int slot = 0;
+        const uint8_t* codes = ring + half * lay.codes + row * 128;
+        const uint8_t* xs = ring + 2 * lay.codes + half * 4 * St::kXBox;
+        const uint8_t* scales = ring + lay.scales + (half * St::kGroups / 2 * rows + row) * (int)sizeof(S);
+        const uint8_t* zeros = ring + lay.zeros + half * St::kGroups / 2 * rows + row;
+        int slot = 0, off = 0;
         uint32_t phase = 0;
         for (int k = 0; k < mine; ++k) {
             if (!tc::mbar_wait(&full[slot], phase, abort, &g_err_q4, 1u)) break;
-            const uint8_t* from = ring + slot * St::kPitch;
-            // (a second block beyond the last has x, codes and scales of zero)
+            // two blocks of 128 columns (those beyond the last have x, codes and
+            // scales of zero)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint4 w[MT][2];
+            for (int blk = 0; blk < 2; ++blk) {
+                uint4 w[2];
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        w[i][h] = *reinterpret_cast<const uint4*>(from + at + (2 * i + h) * 1024 + swz[half]);
-                const S* scales = reinterpret_cast<const S*>(from + St::kScales) + half * kGroups * kRows + sat;
-                const uint8_t* zeros = from + St::kZeros + half * kGroups * kRows + sat;
-                const uint8_t* xs = from + St::kX + half * 2 * St::kXBox;
-                float part[MT][NT][4];
+                for (int h = 0; h < 2; ++h) w[h] = *reinterpret_cast<const uint4*>(codes + off + h * 1024 + swz[blk]);
+                float part[NT][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     uint4 xv[NT];
 #pragma unroll
                     for (int c = 0; c < NT; ++c)
-                        xv[c] = *reinterpret_cast<const uint4*>(xs + (j >> 1) * St::kXBox + c * 1024 + xat[j & 1]);
+                        xv[c] = *reinterpret_cast<const uint4*>(xs + off + (2 * blk + (j >> 1)) * St::kXBox + c * 1024 +
+                                                                xat[j & 1]);
                     constexpr int kSteps = GROUP / 32;           // steps of a group
+                    const int group = (4 * blk + j) / kSteps;
+                    uint32_t r[2][4];
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        uint32_t r[2][4];
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t word = j == 0 ? w[h].x : j == 1 ? w[h].y : j == 2 ? w[h].z : w[h].w;
+                        OP::unpack(word, ZEROS ? zeros[off + group * rows + 8 * h] : 8u, r[h]);
+                    }
+#pragma unroll
+                    for (int c = 0; c < NT; ++c) {
+                        if (j % kSteps == 0) OP::mma_first(part[c], r[0][0], r[1][0], r[0][1], r[1][1], xv[c].x, xv[c].y);
+                        else OP::mma(part[c], r[0][0], r[1][0], r[0][1], r[1][1], xv[c].x, xv[c].y);
+                        OP::mma(part[c], r[0][2], r[1][2], r[0][3], r[1][3], xv[c].z, xv[c].w);
+                    }
+                    if ((j + 1) % kSteps == 0) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const uint32_t word = j == 0 ? w[i][h].x : j == 1 ? w[i][h].y : j == 2 ? w[i][h].z : w[i][h].w;
-                            OP::unpack(word, ZEROS ? zeros[j / kSteps * kRows + 16 * i + 8 * h] : 8u, r[h]);
-                        }
+                            const float s = el::to_f32(
+                                *reinterpret_cast<const S*>(scales + off + (group * rows + 8 * h) * (int)sizeof(S)));
 #pragma unroll
-                        for (int c = 0; c < NT; ++c) {
-                            if (j % kSteps == 0) OP::mma_first(part[i][c], r[0][0], r[1][0], r[0][1], r[1][1], xv[c].x, xv[c].y);
-                            else OP::mma(part[i][c], r[0][0], r[1][0], r[0][1], r[1][1], xv[c].x, xv[c].y);
-                            OP::mma(part[i][c], r[0][2], r[1][2], r[0][3], r[1][3], xv[c].z, xv[c].w);
-                        }
-                        if ((j + 1) % kSteps == 0) {
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const float s = el::to_f32(scales[j / kSteps * kRows + 16 * i + 8 * h]);
-#pragma unroll
-                                for (int c = 0; c < NT; ++c) {
-                                    acc[i][c][2 * h] = fmaf(s, part[i][c][2 * h], acc[i][c][2 * h]);
-                                    acc[i][c][2 * h + 1] = fmaf(s, part[i][c][2 * h + 1], acc[i][c][2 * h + 1]);
-                                }
+                            for (int c = 0; c < NT; ++c) {
+                                acc[c][2 * h] = fmaf(s, part[c][2 * h], acc[c][2 * h]);
+                                acc[c][2 * h + 1] = fmaf(s, part[c][2 * h + 1], acc[c][2 * h + 1]);
                             }
                         }
                     }
@@ -350,36 +373,41 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             }
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&empty[slot]);
-            if (++slot == DEPTH) {
-                slot = 0;
+            off += lay.pitch;
+            if (++slot == a.depth) {
+                slot = off = 0;
                 phase ^= 1;
             }
         }
     }
     __syncthreads();                                              // the ring is free
-    float(*sums)[kRows + 1] = reinterpret_cast<float(*)[kRows + 1]>(ring);
-    if (warp < WARPS) {
+    // sums[half][column][row]
+    float* sums = reinterpret_cast<float*>(ring);
+    const int pitch = rows + 1;
+    if (warp < warps) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int c = 0; c < NT; ++c)
 #pragma unroll
-            for (int c = 0; c < NT; ++c)
-#pragma unroll
-                for (int u = 0; u < 4; ++u)      // column 2 t + u of eight, t or t + 4 of the vectors
-                    sums[8 * c + t + 4 * (u & 1)][16 * (MT * warp + i) + 8 * (u >> 1) + rho] = acc[i][c][u];
+            for (int u = 0; u < 4; ++u)      // column 2 t + u of eight, t or t + 4 of the vectors
+                sums[(half * kCols + 8 * c + t + 4 * (u & 1)) * pitch + row + 8 * (u >> 1)] = acc[c][u];
     }
     if (a.split > 1) cluster_sync();
     else __syncthreads();
-    const int used = min(a.cols - col0, kCols) / PARTS;           // vectors of this tile
-    for (int e = rank * (WARPS * 32 + 32) + threadIdx.x; e < used * kRows; e += a.split * (WARPS * 32 + 32)) {
-        const int v = e / kRows, r = e % kRows;
+    const int used = min(a.cols - col0, used_cols(NT, PARTS)) / PARTS;      // vectors of this tile
+    for (int e = rank * threads + threadIdx.x; e < used * rows; e += a.split * threads) {
+        const int v = e / rows, r = e % rows;
         if (row0 + r >= a.m) continue;
         float sum = 0.f;
 #pragma unroll
         for (int p = PARTS - 1; p >= 0; --p) {                    // the smallest part first
-            if (a.split > 1)
-                for (int w = 0; w < a.split; ++w) sum += cluster_load(&sums[v * PARTS + p][r], w);
-            else
-                sum += sums[v * PARTS + p][r];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const float* at = &sums[(q * kCols + v * PARTS + p) * pitch + r];
+                if (a.split > 1)
+                    for (int w = 0; w < a.split; ++w) sum += cluster_load(at, w);
+                else
+                    sum += *at;
+            }
         }
         const int64_t o = (int64_t)(col0 / PARTS + v) * a.m + row0 + r;
         if (PARTS > 1 || a.wide) {
@@ -453,50 +481,74 @@ constexpr CUtensorMapDataType map_type(float) { return CU_TENSOR_MAP_DATA_TYPE_F
 constexpr CUtensorMapDataType map_type(__half) { return CU_TENSOR_MAP_DATA_TYPE_FLOAT16; }
 constexpr CUtensorMapDataType map_type(bf16) { return CU_TENSOR_MAP_DATA_TYPE_BFLOAT16; }
 
-template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NT, int MT, int WARPS, int DEPTH, int RESIDENT>
+constexpr int kSmemOfSm = 227 * 1024;
+
+// Groups of rows of a tile and blocks of a cluster: what takes the shortest by a
+// model of a multiprocessor's time, in units of what it takes for 16 rows and a
+// stage (0.11 us).  A block needs five such a stage at least however few its rows
+// are (the latency of its warps' chain), and sixteen to start and to end.
+inline void choose_tile(ApplyArgs* a, int chunks, int most) {
+    const int stages = (int)((a->blocks + 3) / 4), sms = sm_count();
+    double best = 1e300;
+    for (int R = most; R >= 1; --R) {
+        const int64_t tiles = ((a->m + 15) / 16 + R - 1) / R * chunks;
+        const int slots = (R > 4 ? 1 : 2) * sms;
+        for (int split = 1; split <= 8 && split <= stages; split += split < 4 ? 1 : 2) {
+            const double blocks = (double)tiles * split;
+            const double waves = ceil(blocks / slots), beside = blocks < slots ? ceil(blocks / sms) : slots / sms;
+            const double cost = waves * (fmax(beside * R, 5.) * ((stages + split - 1) / split) + 16.);
+            if (cost < best) {
+                best = cost;
+                a->R = R;
+                a->split = split;
+            }
+        }
+    }
+}
+
+template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NT>
 lrc_status apply_launch(ApplyArgs a, cudaStream_t s) {
-    using St = StageOf<S, GROUP, ZEROS, NT, MT, WARPS>;
-    constexpr int kCols = St::kCols, kRows = St::kRows;
-    static_assert(kCols % PARTS == 0, "whole vectors a tile");
-    a.xrows = a.cols < kCols ? a.cols : kCols;
+    using St = StageOf<S, GROUP, ZEROS, NT>;
+    constexpr int kUsed = used_cols(NT, PARTS);
+    a.xrows = a.cols < kUsed ? a.cols : kUsed;
+    const int chunks = (a.cols + kUsed - 1) / kUsed;
+    choose_tile(&a, chunks, most_rows(NT));
+    const uint32_t rows = 16 * a.R;
+    const St lay(a.R);
+    const int room = kSmemOfSm / (a.R > 4 ? 1 : 2) - 3072;
+    a.depth = room / lay.pitch < kMostDepth ? room / lay.pitch : kMostDepth;
     CUtensorMap qm, xm, sm, zm{};
-    lrc_status st = encode_map_2d(&qm, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.Q, a.blocks * 64, a.m, a.blocks * 64, 128, kRows,
+    lrc_status st = encode_map_2d(&qm, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.Q, a.blocks * 64, a.m, a.blocks * 64, 128, rows,
                                   true, "Q");
     if (st != LRC_OK) return st;
     st = encode_map_2d(&xm, map_type(typename OP::type()), a.x, a.xcols, a.cols, a.ldx * 2, 64, (uint32_t)a.xrows, true,
                        "X");
     if (st != LRC_OK) return st;
-    st = encode_map_2d(&sm, map_type(S()), a.scales, a.m, a.groups, a.ldm * (int64_t)sizeof(S), kRows, St::kGroups, false,
+    st = encode_map_2d(&sm, map_type(S()), a.scales, a.m, a.groups, a.ldm * (int64_t)sizeof(S), rows, St::kGroups, false,
                        "scales");
     if (st != LRC_OK) return st;
     if (ZEROS) {
-        st = encode_map_2d(&zm, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.zeros, a.m, a.groups, a.ldm, kRows, St::kGroups, false,
+        st = encode_map_2d(&zm, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.zeros, a.m, a.groups, a.ldm, rows, St::kGroups, false,
                            "zeros");
         if (st != LRC_OK) return st;
     }
-    // Blocks that share a tile's columns: the number that fills the
-    // multiprocessors' waves best, a wave's fixed part taken as four stages.
-    const int64_t tiles = (a.m + kRows - 1) / kRows, chunks = (a.cols + kCols - 1) / kCols, pairs = (a.blocks + 1) / 2;
-    const int64_t slots = (int64_t)RESIDENT * sm_count();
-    int64_t best = INT64_MAX;
-    for (int split = 1; split <= 8 && split <= pairs; ++split) {
-        const int64_t cost = (tiles * chunks * split + slots - 1) / slots * ((pairs + split - 1) / split + 4);
-        if (cost < best) {
-            best = cost;
-            a.split = split;
-        }
-    }
     unsigned grid;
-    if ((st = grid_of(tiles * a.split, 1, "lrc_q4_apply", &grid)) != LRC_OK) return st;
-    auto kernel = q4_apply_kernel<OP, S, PARTS, GROUP, ZEROS, NT, MT, WARPS, DEPTH, RESIDENT>;
-    constexpr int kSmem = DEPTH * St::kPitch + 1024;
-    static_assert(St::kSums <= DEPTH * St::kPitch, "the sums lie in the ring");
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if ((st = grid_of((a.m + rows - 1) / rows * a.split, 1, "lrc_q4_apply", &grid)) != LRC_OK) return st;
+    auto kernel = q4_apply_kernel<OP, S, PARTS, GROUP, ZEROS, NT>;
+    const int smem = a.depth * lay.pitch + 1024;
+    // the attribute is the device's: set once on each
+    static std::atomic<uint64_t> set_on{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && (dev >= 64 || !(set_on.load() >> dev & 1))) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemOfSm - 1024);
+        if (e == cudaSuccess && dev < 64) set_on |= (uint64_t)1 << dev;
+    }
     if (e != cudaSuccess) return cuda_fail(e, "q4_apply_kernel");
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(grid, (unsigned)chunks);
-    cfg.blockDim = dim3(WARPS * 32 + 32);
-    cfg.dynamicSmemBytes = kSmem;
+    cfg.blockDim = dim3(64 * a.R + 32);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -511,29 +563,27 @@ lrc_status apply_launch(ApplyArgs a, cudaStream_t s) {
     return after_launch("q4_apply_kernel");
 }
 
-template <typename OP, typename S, int PARTS, int NT, int MT, int WARPS, int DEPTH, int RESIDENT>
+template <typename OP, typename S, int PARTS, int NT>
 lrc_status apply_groups(const ApplyArgs& a, int group, cudaStream_t s) {
     if (a.zeros) {
-        if (group == 32) return apply_launch<OP, S, PARTS, 32, true, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
-        if (group == 64) return apply_launch<OP, S, PARTS, 64, true, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
-        return apply_launch<OP, S, PARTS, 128, true, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
+        if (group == 32) return apply_launch<OP, S, PARTS, 32, true, NT>(a, s);
+        if (group == 64) return apply_launch<OP, S, PARTS, 64, true, NT>(a, s);
+        return apply_launch<OP, S, PARTS, 128, true, NT>(a, s);
     }
-    if (group == 32) return apply_launch<OP, S, PARTS, 32, false, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
-    if (group == 64) return apply_launch<OP, S, PARTS, 64, false, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
-    return apply_launch<OP, S, PARTS, 128, false, NT, MT, WARPS, DEPTH, RESIDENT>(a, s);
+    if (group == 32) return apply_launch<OP, S, PARTS, 32, false, NT>(a, s);
+    if (group == 64) return apply_launch<OP, S, PARTS, 64, false, NT>(a, s);
+    return apply_launch<OP, S, PARTS, 128, false, NT>(a, s);
 }
 
-#define Q4V 1, 16, 3, 1
+// The narrowest tiles of columns that take the vectors in as few passes over the
+// codes as the widest would.
 template <typename OP, typename S, int PARTS>
 lrc_status apply_tiles(const ApplyArgs& a, int group, cudaStream_t s) {
-    if constexpr (PARTS == 1) {
-        if (a.cols <= 8) return apply_groups<OP, S, 1, 1, Q4V>(a, group, s);
-        if (a.cols <= 16) return apply_groups<OP, S, 1, 2, 1, 8, 4, 2>(a, group, s);
-        if (a.cols <= 32) return apply_groups<OP, S, 1, 4, 1, 8, 2, 2>(a, group, s);
-        return apply_groups<OP, S, 1, 8, 1, 8, 3, 1>(a, group, s);
-    } else {
-        return apply_groups<OP, S, 3, 3, 1, 8, 3, 2>(a, group, s);
-    }
+    const int passes = (a.cols + used_cols(4, PARTS) - 1) / used_cols(4, PARTS);
+    if (used_cols(1, PARTS) * passes >= a.cols) return apply_groups<OP, S, PARTS, 1>(a, group, s);
+    if (used_cols(2, PARTS) * passes >= a.cols) return apply_groups<OP, S, PARTS, 2>(a, group, s);
+    if (used_cols(3, PARTS) * passes >= a.cols) return apply_groups<OP, S, PARTS, 3>(a, group, s);
+    return apply_groups<OP, S, PARTS, 4>(a, group, s);
 }
 
 template <typename OP, typename S, typename Y, int PARTS>
