@@ -236,9 +236,9 @@ struct StageOf {
     }
 };
 
-// Groups of 16 rows of a tile at most (17 warps of a block have 96 registers a
-// thread, 13 have 128).
-constexpr int most_rows(int NT) { return NT > 2 ? 6 : 8; }
+// Groups of 16 rows of a tile at most: 15 warps of a block have 128 registers a
+// thread, 17 would have 96.
+constexpr int kMostRows = 7;
 // Columns of B that a tile uses: whole vectors.
 constexpr int used_cols(int NT, int PARTS) { return 8 * NT / PARTS * PARTS; }
 constexpr int kMostDepth = 8;      // stages of a ring
@@ -246,7 +246,7 @@ constexpr int kMostDepth = 8;      // stages of a ring
 // OP: the instructions' element type; S: the scales' type; PARTS: columns of B
 // that make one vector (3: a binary32 vector as hi + mid + lo in bfloat16).
 template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NT>
-__global__ void __launch_bounds__(64 * most_rows(NT) + 32, 1)
+__global__ void __launch_bounds__(64 * kMostRows + 32, 1)
 q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap xmap,
                 const __grid_constant__ CUtensorMap smap, const __grid_constant__ CUtensorMap zmap,
                 const __grid_constant__ ApplyArgs a) {
@@ -487,10 +487,10 @@ constexpr int kSmemOfSm = 227 * 1024;
 // model of a multiprocessor's time, in units of what it takes for 16 rows and a
 // stage (0.11 us).  A block needs five such a stage at least however few its rows
 // are (the latency of its warps' chain), and sixteen to start and to end.
-inline void choose_tile(ApplyArgs* a, int chunks, int most) {
+inline void choose_tile(ApplyArgs* a, int chunks) {
     const int stages = (int)((a->blocks + 3) / 4), sms = sm_count();
     double best = 1e300;
-    for (int R = most; R >= 1; --R) {
+    for (int R = kMostRows; R >= 1; --R) {
         const int64_t tiles = ((a->m + 15) / 16 + R - 1) / R * chunks;
         const int slots = (R > 4 ? 1 : 2) * sms;
         for (int split = 1; split <= 8 && split <= stages; split += split < 4 ? 1 : 2) {
@@ -512,7 +512,7 @@ lrc_status apply_launch(ApplyArgs a, cudaStream_t s) {
     constexpr int kUsed = used_cols(NT, PARTS);
     a.xrows = a.cols < kUsed ? a.cols : kUsed;
     const int chunks = (a.cols + kUsed - 1) / kUsed;
-    choose_tile(&a, chunks, most_rows(NT));
+    choose_tile(&a, chunks);
     const uint32_t rows = 16 * a.R;
     const St lay(a.R);
     const int room = kSmemOfSm / (a.R > 4 ? 1 : 2) - 3072;
