@@ -432,15 +432,15 @@ lrc_status lrc_device_status(lrc_stream_t stream) {
     const uint32_t t3 = take_tt3_tc_error();
     const uint32_t tn = take_ttn_tc_error();
     const uint32_t sk = take_skinny_error() | take_split_error() | take_split32_error();
-    const uint32_t q4 = take_q4_error();
+    const uint32_t q4 = take_q4_error(), ln = take_norm_error();
     const uint32_t t = t1 | t3 | tn;
-    if (q4 == 0xffffffffu || a == 0xffffffffu || t1 == 0xffffffffu || t3 == 0xffffffffu || tn == 0xffffffffu || sk == 0xffffffffu) {
+    if (q4 == 0xffffffffu || ln == 0xffffffffu || a == 0xffffffffu || t1 == 0xffffffffu || t3 == 0xffffffffu || tn == 0xffffffffu || sk == 0xffffffffu) {
         set_error("could not read the device error words");
         return LRC_ERR_CUDA;
     }
-    if (a | t | sk | q4) {
+    if (a | t | sk | q4 | ln) {
         set_error("a bounded device wait gave up (apply code 0x%x, TT code 0x%x, small-batch apply code 0x%x, "
-                  "4-bit product code 0x%x)", a, t, sk, q4);
+                  "4-bit product code 0x%x, layer norm code 0x%x)", a, t, sk, q4, ln);
         return LRC_ERR_TIMEOUT;
     }
     return LRC_OK;

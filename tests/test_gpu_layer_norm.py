@@ -112,7 +112,7 @@ def grad_bounds(dy, x, gamma, mu, r, want, out):
             kr * dy.double().abs().sum(0))
 
 
-@pytest.mark.parametrize("rows,cols", SHAPES + [(700, 129), (1025, 64)])
+@pytest.mark.parametrize("rows,cols", SHAPES + [(700, 129), (1025, 64), (1300, 9000), (700, 20001), (1901, 4097)])
 @pytest.mark.parametrize("fmt,pfmt", [("f32", "f32"), ("f16", "f16"), ("f16_o16", "f16"), ("bf16", "f32"), ("bf16", None)])
 @pytest.mark.parametrize("pad,shift", [(0, 0), (3, 1)])
 def test_grad(lrc, cuda, rows, cols, fmt, pfmt, pad, shift):
