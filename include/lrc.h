@@ -652,7 +652,7 @@ LRC_API lrc_status lrc_layer_norm_grad(const void* dY, const void* X, const void
  *           of `tfmt`) and their places in the row, int64, row pitch ldt.  An
  *           entry with an index outside [0, V) is absent, as is one with the
  *           logit -infinity.  The same place may be named more than once.
- *           1 <= K <= 1024, else LRC_ERR_UNSUPPORTED
+ *           1 <= K <= 1024, else LRC_ERR_UNSUPPORTED; V at most 2^30
  *   w       device, rows binary32 weights; NULL for ones
  *   loss    device, rows binary32 values; NULL where not wanted
  *   lse     device, rows binary32 values log sum_j exp(z_j / tau); NULL where

@@ -432,15 +432,15 @@ lrc_status lrc_device_status(lrc_stream_t stream) {
     const uint32_t t3 = take_tt3_tc_error();
     const uint32_t tn = take_ttn_tc_error();
     const uint32_t sk = take_skinny_error() | take_split_error() | take_split32_error();
-    const uint32_t q4 = take_q4_error(), ln = take_norm_error();
+    const uint32_t q4 = take_q4_error(), ln = take_norm_error(), ds = take_distill_error();
     const uint32_t t = t1 | t3 | tn;
-    if (q4 == 0xffffffffu || ln == 0xffffffffu || a == 0xffffffffu || t1 == 0xffffffffu || t3 == 0xffffffffu || tn == 0xffffffffu || sk == 0xffffffffu) {
+    if (q4 == 0xffffffffu || ln == 0xffffffffu || ds == 0xffffffffu || a == 0xffffffffu || t1 == 0xffffffffu || t3 == 0xffffffffu || tn == 0xffffffffu || sk == 0xffffffffu) {
         set_error("could not read the device error words");
         return LRC_ERR_CUDA;
     }
-    if (a | t | sk | q4 | ln) {
+    if (a | t | sk | q4 | ln | ds) {
         set_error("a bounded device wait gave up (apply code 0x%x, TT code 0x%x, small-batch apply code 0x%x, "
-                  "4-bit product code 0x%x, layer norm code 0x%x)", a, t, sk, q4, ln);
+                  "4-bit product code 0x%x, layer norm code 0x%x, distillation code 0x%x)", a, t, sk, q4, ln, ds);
         return LRC_ERR_TIMEOUT;
     }
     return LRC_OK;
@@ -570,6 +570,7 @@ lrc_status check_distill(const void* Z, const void* T, const int64_t* idx, const
     if (!(t > 0.f) || isinf(t)) return invalid("tau = %g must be positive and finite in binary32", tau);
     if (isinf(1.f / t)) return invalid("tau = %g is too small", tau);
     if (K > distill_max_top()) return unsupported("more than 1024 teacher entries a row");
+    if (V > 1 << 30) return unsupported("more than 2^30 logits a row");
     if (rows == 0) return LRC_OK;
     if (!Z || !T || !idx) return invalid("null pointer");
     if (!aligned_to(Z, storage_bytes((lrc_fmt)fmt))) return misaligned_element("Z");

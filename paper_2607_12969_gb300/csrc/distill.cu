@@ -1,29 +1,37 @@
 // distill.cu -- distillation from a teacher's top logits (lrc_distill,
 // lrc_distill_grad), binary32 arithmetic.
 //
-// With z' = z / tau, the row's log-sum-exp L and the teacher's p:
+// With z' = z / tau, the row's log-sum-exp L of z' and the teacher's p:
 //   loss = tau^2 w sum_k p_k (log p_k - (z'_{i_k} - L)),
 //   dz_j = tau w g (exp(z'_j - L) - sum over k with i_k = j of p_k).
+//
+// Bound by HBM (a row is read once and its gradient written once) and, with both
+// the sum and the gradient, nearly by the exponentials, two an element at 16 a
+// clock on a multiprocessor.
+//
+// Persistent blocks, one row at a time (or a cluster a row where rows are few, each
+// block a slice).  One warp brings the row in chunks by bulk copies into a ring in
+// shared memory, another one prepares the next row's teacher entries, the others
+// form the running maximum and sum chunk by chunk as they come and, where the row
+// fits into the ring, the gradient from the same copy; else the chunks come again
+// (from L2).  The ring holds the next row's first chunks by then.  At the places of
+// the teacher's entries the gradient is written once more at the end of the row.
+#include <math.h>
+
 #include "common.cuh"
 #include "elem.cuh"
+#include "tc.cuh"
 
 namespace lrc {
 namespace {
 
 using bf16 = __nv_bfloat16;
 
-constexpr int kThreads = 256;
-constexpr int kMaxTop = 1024;
+__device__ unsigned int g_err_distill;
 
-__device__ __forceinline__ float block_all(float x, float* sh, bool maximum) {
-    x = maximum ? el::warp_max(x) : el::warp_sum(x);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
-    __syncthreads();
-    x = sh[0];
-    for (int i = 1; i < (int)blockDim.x / 32; ++i) x = maximum ? fmaxf(x, sh[i]) : x + sh[i];
-    return x;
-}
+constexpr int kMaxTop = 1024;
+constexpr int kMostChunks = 32;
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct Args {
     const void* Z;
@@ -35,93 +43,496 @@ struct Args {
     float* loss;
     float* lse_out;
     void* dZ;
-    int64_t V, K, ldz, ldt, lddz;
+    int64_t rows, V, ldz, ldt, lddz, slice;
+    int K, table;            // teacher entries; places of the table that finds repeated ones
+    int chunks;              // of the ring
+    bool keep;               // the slice stays in the ring until its gradient is written
     float tau;
     int tkind;
 };
 
-// One block a row.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) distill_kernel(Args a) {
-    __shared__ float sh[kThreads / 32];
-    __shared__ float p[kMaxTop];
-    __shared__ int64_t at[kMaxTop];
-    const int64_t row = blockIdx.x;
-    const T* z = static_cast<const T*>(a.Z) + row * a.ldz;
-    const float it = 1.f / a.tau;
-    // the row's log-sum-exp
-    float L;
-    if (a.lse_in) {
-        L = a.lse_in[row];
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// The larger one; a NaN where there is one.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+
+// 16 bytes of elements (kVec of them) as binary32 and back.
+template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
+__device__ __forceinline__ void widen(const uint4& a, float (&v)[4], float) {
+    v[0] = __uint_as_float(a.x), v[1] = __uint_as_float(a.y), v[2] = __uint_as_float(a.z), v[3] = __uint_as_float(a.w);
+}
+__device__ __forceinline__ void widen(const uint4& a, float (&v)[8], __half) {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        v[2 * i] = f.x, v[2 * i + 1] = f.y;
+    }
+}
+__device__ __forceinline__ void widen(const uint4& a, float (&v)[8], bf16) {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+}
+__device__ __forceinline__ uint4 narrow(const float (&v)[4], float) {
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+__device__ __forceinline__ uint4 narrow(const float (&v)[8], __half) {
+    return make_uint4(tc::pack_half2(v[0], v[1]), tc::pack_half2(v[2], v[3]), tc::pack_half2(v[4], v[5]),
+                      tc::pack_half2(v[6], v[7]));
+}
+__device__ __forceinline__ uint4 narrow(const float (&v)[8], bf16) {
+    return make_uint4(tc::pack_bf162(v[0], v[1]), tc::pack_bf162(v[2], v[3]), tc::pack_bf162(v[4], v[5]),
+                      tc::pack_bf162(v[6], v[7]));
+}
+
+// Running maximum and sum of exp2((z - m) k): m = -infinity has s = 0; a NaN or
+// +infinity makes s NaN.
+struct Running {
+    float m = -INFINITY, s = 0.f, shift = 0.f;       // shift = -m k, 0 for m = -infinity
+    __device__ __forceinline__ void raise(float to, float k) {
+        const float mm = max_nan(m, to);
+        if (mm != m) {                               // (a NaN too)
+            s *= ex2((m - mm) * k);
+            m = mm;
+            shift = -mm * k;
+        }
+    }
+    __device__ __forceinline__ void join(float om, float os, float k) {
+        const float mm = max_nan(m, om);
+        s = (m == mm ? s : s * ex2((m - mm) * k)) + (om == mm ? os : os * ex2((om - mm) * k));
+        m = mm;
+    }
+};
+
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_store(float* p, uint32_t rank, float v) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(p)), "r"(rank));
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive(uint64_t* bar, uint32_t rank) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(bar)), "r"(rank));
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at) : "memory");
+}
+// (Within a limit of time, like every wait of the kernel.)
+__device__ __forceinline__ void cluster_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
+    const uint64_t t0 = tc::globaltimer();
+    while (true) {
+        uint32_t ok;
+        asm volatile(
+            "{\n .reg .pred p;\n"
+            " mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+            " selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(ok) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
+        if (ok || *abort) return;
+        if (tc::globaltimer() - t0 > tc::kWaitLimitNs) {
+            atomicOr(&g_err_distill, 2u);
+            *abort = 1;
+            return;
+        }
+    }
+}
+
+// What the teacher's warp leaves for a row.
+struct Teacher {
+    float c;                 // tau w g, 0 where the row has no gradient
+    float lw;                // tau^2 w, 0 where the row has no loss
+    int repeated;            // some place is named more than once
+};
+
+// Shared memory: ring | per row parity: at, p, log p, z of the K entries | table.
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS + 64, 512 / THREADS) distill_kernel(const __grid_constant__ Args a) {
+    constexpr int kChunk = THREADS * 32;                      // bytes: two vectors a thread
+    constexpr int kWarps = THREADS / 32, N = kVec<T>;
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ uint64_t full[kMostChunks], empty[kMostChunks], tfull[2], tempty[2], got[2];
+    __shared__ float part_m[2][kWarps], part_s[2][kWarps];    // [row parity][warp]
+    __shared__ float all_m[2][8], all_s[2][8];                // [row parity][block of the cluster]
+    __shared__ Teacher teacher[2];
+    __shared__ int abort_flag;
+    int* at = reinterpret_cast<int*>(ring + a.chunks * kChunk);          // [2][K]
+    float* pk = reinterpret_cast<float*>(at + 2 * a.K);
+    float* lpk = pk + 2 * a.K;
+    float* zk = lpk + 2 * a.K;
+    int* table = reinterpret_cast<int*>(zk + 2 * a.K);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t ranks = cluster_size(), rank = cluster_rank();
+    const int clusters = gridDim.x / ranks, first = blockIdx.x / ranks;
+    const int64_t c0 = rank * a.slice;
+    const int len = (int)min(a.slice, a.V - c0);              // elements of this block's slice
+    const int mine = first < a.rows ? ((int)a.rows - first + clusters - 1) / clusters : 0;
+    const T* Z = static_cast<const T*>(a.Z) + c0;
+    T* dZ = a.dZ ? static_cast<T*>(a.dZ) + c0 : nullptr;
+    const bool sums = a.lse_in == nullptr;
+    const float it = 1.f / a.tau, k2 = kLog2e * it;
+    volatile int* abort = &abort_flag;
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (int d = 0; d < a.chunks; ++d) {
+            tc::mbar_init(&full[d], 1);
+            tc::mbar_init(&empty[d], kWarps);
+        }
+        for (int p = 0; p < 2; ++p) {
+            tc::mbar_init(&tfull[p], 1);
+            tc::mbar_init(&tempty[p], kWarps);
+            tc::mbar_init(&got[p], ranks);
+        }
+        tc::fence_barrier_init();
+    }
+    if (ranks > 1) cluster_sync();                            // every block's barriers are there
+    else __syncthreads();
+    tc::pdl_wait();
+    tc::pdl_trigger();
+    // A row's slice: `head` elements up to a 16-byte boundary, nvec vectors, the rest.
+    auto head_of = [&](const T* z) {
+        return min((uint32_t)len, (16u - (uint32_t)(reinterpret_cast<uintptr_t>(z) & 15u)) % 16u / (uint32_t)sizeof(T));
+    };
+
+    if (warp == kWarps) {
+        // ---- the copies
+        if (lane == 0) {
+            int slot = 0;
+            uint32_t phase = 1, used = 0;
+            bool go = true;
+            for (int r = 0; r < mine && go; ++r) {
+                const T* z = Z + (first + (int64_t)r * clusters) * a.ldz;
+                const uint32_t head = head_of(z), bytes = (len - head) / N * 16;
+                const uint8_t* src = reinterpret_cast<const uint8_t*>(z + head);
+                const int times = sums && dZ && !a.keep ? 2 : 1;
+                for (int pass = 0; pass < times && go; ++pass)
+                    for (uint32_t o = 0; o < bytes; o += kChunk) {
+                        if (used >= (uint32_t)a.chunks &&
+                            !tc::mbar_wait(&empty[slot], phase, abort, &g_err_distill, 1u)) {
+                            go = false;
+                            break;
+                        }
+                        const uint32_t n = min(bytes - o, (uint32_t)kChunk);
+                        tc::mbar_arrive_expect_tx(&full[slot], n);
+                        tc::bulk_load(ring + slot * kChunk, src + o, n, &full[slot]);
+                        ++used;
+                        if (++slot == a.chunks) {
+                            slot = 0;
+                            phase ^= 1;
+                        }
+                    }
+            }
+            // no copy is in flight when the block ends
+            volatile int no_abort = 0;
+            for (uint32_t u = used > (uint32_t)a.chunks ? used - a.chunks : 0; u < used; ++u)
+                tc::mbar_wait(&full[u % a.chunks], u / a.chunks & 1, &no_abort, &g_err_distill, 1u);
+        }
+        __syncwarp();
+    } else if (warp == kWarps + 1) {
+        // ---- the teacher's entries, a row ahead
+        const float none = -INFINITY;
+        for (int r = 0; r < mine; ++r) {
+            const int p = r & 1;
+            if (r >= 2) tc::mbar_wait(&tempty[p], (r >> 1 & 1) ^ 1, abort, &g_err_distill, 1u);
+            __syncwarp();
+            const int64_t row = first + (int64_t)r * clusters;
+            const T* z = static_cast<const T*>(a.Z) + row * a.ldz;
+            int* my_at = at + p * a.K;
+            float *my_p = pk + p * a.K, *my_lp = lpk + p * a.K, *my_z = zk + p * a.K;
+            float top = none;
+#pragma unroll 2
+            for (int k = lane; k < a.K; k += 32) {
+                const int64_t i = __ldg(a.idx + row * a.ldt + k);
+                const bool there = i >= 0 && i < a.V;
+                const float t = there ? el::load_as(a.T, a.tkind, row * a.ldt + k) * it : none;
+                const bool in = t != none;                    // (a NaN is)
+                my_at[k] = in ? (int)i : -1;
+                my_z[k] = in ? el::to_f32(z[i]) : 0.f;
+                my_p[k] = t;
+                top = max_nan(top, t);
+            }
+            const float w = a.w ? __ldg(a.w + row) : 1.f, g = a.g ? __ldg(a.g + row) : 1.f;
+            for (int e = lane; e < a.table; e += 32) table[e] = -1;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+            float s = 0.f;
+            for (int k = lane; k < a.K; k += 32) s += expf(my_p[k] - top);
+            s = el::warp_sum(s);
+            const float lt = top + logf(s);
+            int repeated = 0;
+            __syncwarp();
+            for (int k = lane; k < a.K; k += 32) {
+                const int i = my_at[k];
+                const float lp = my_p[k] - lt;
+                my_lp[k] = lp;
+                my_p[k] = i < 0 ? 0.f : expf(lp);
+                if (i >= 0) {
+                    uint32_t h = (uint32_t)i * 2654435761u >> 16;
+                    while (true) {                            // (the table has twice as many places)
+                        h &= a.table - 1;
+                        const int was = atomicCAS(&table[h], -1, i);
+                        if (was == i) repeated = 1;
+                        if (was == i || was == -1) break;
+                        ++h;
+                    }
+                }
+            }
+            repeated = __any_sync(0xffffffffu, repeated);
+            if (lane == 0) {
+                const bool on = top != none && w != 0.f;
+                teacher[p].c = on && g != 0.f ? a.tau * w * g : 0.f;
+                teacher[p].lw = on ? a.tau * a.tau * w : 0.f;
+                teacher[p].repeated = repeated;
+            }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&tfull[p]);
+        }
     } else {
-        float top = -INFINITY;
-        bool odd = false;
-        for (int64_t j = threadIdx.x; j < a.V; j += kThreads) {
-            const float v = el::to_f32(z[j]);
-            odd |= v != v;
-            top = fmaxf(top, v);
-        }
-        top = block_all(top, sh, true);
-        const float m = top == -INFINITY ? 0.f : top;
-        float s = 0.f;
-        for (int64_t j = threadIdx.x; j < a.V; j += kThreads) s += expf((el::to_f32(z[j]) - m) * it);
-        s = block_all(odd ? NAN : s, sh, false);
-        L = m * it + logf(s);
-        if (a.lse_out && threadIdx.x == 0) a.lse_out[row] = L;
-    }
-    // the teacher's probabilities
-    float tt = -INFINITY;
-    for (int64_t k = threadIdx.x; k < a.K; k += kThreads) {
-        const int64_t i = a.idx[row * a.ldt + k];
-        const bool there = i >= 0 && i < a.V;
-        at[k] = there ? i : -1;
-        p[k] = there ? el::load_as(a.T, a.tkind, row * a.ldt + k) * it : -INFINITY;
-        tt = fmaxf(tt, p[k] != p[k] ? INFINITY : p[k]);
-    }
-    tt = block_all(tt, sh, true);
-    const float w = a.w ? a.w[row] : 1.f;
-    const float up = a.g ? a.g[row] : 1.f;
-    const bool on = tt > -INFINITY && w != 0.f;
-    float s = 0.f;
-    for (int64_t k = threadIdx.x; k < a.K; k += kThreads) s += expf(p[k] - tt);
-    s = block_all(s, sh, false);
-    const float lt = tt + logf(s);
-    float kl = 0.f;
-    for (int64_t k = threadIdx.x; k < a.K; k += kThreads) {
-        const float lp = p[k] - lt, q = expf(lp);
-        if (q != 0.f) kl += q * (lp - (el::to_f32(z[at[k] < 0 ? 0 : at[k]]) * it - L));
-        p[k] = q;
-    }
-    kl = block_all(kl, sh, false);
-    if (a.loss && threadIdx.x == 0) a.loss[row] = on ? a.tau * a.tau * w * kl : 0.f;
-    if (!a.dZ) return;
-    T* d = static_cast<T*>(a.dZ) + row * a.lddz;
-    const float c = on && up != 0.f ? a.tau * w * up : 0.f;
-    // the places of the teacher's entries are kept apart: d may be z
-    constexpr int kEach = kMaxTop / kThreads;
-    float mine[kEach];
+        // ---- sums and gradient
+        int slot = 0;
+        uint32_t phase = 0;
+        // Elements outside the vectors: lanes 0 ... 7 of the first warp have those before,
+        // 8 ... 15 those after; loaded a row ahead.
+        int edge = -1;
+        float edge_z = 0.f, edge_next = 0.f;
+        auto edge_of = [&](int r, float* v) {
+            if (warp != 0 || r >= mine || lane >= 16) return -1;
+            const T* z = Z + (first + (int64_t)r * clusters) * a.ldz;
+            const uint32_t head = head_of(z), body = (len - head) / N * N;
+            const uint32_t i = lane < 8 ? lane : lane - 8 + head + body;
+            if (i >= (lane < 8 ? head : (uint32_t)len)) return -1;
+            *v = el::to_f32(z[i]);
+            return (int)i;
+        };
+        int edge_at_next = edge_of(0, &edge_next);
+        // Each block gives its maximum and sum to every block of the cluster.  (One that
+        // gives those of row r + 2 has all of row r + 1, which the others gave after they
+        // had read those of row r.  And no block writes a gradient before all have their
+        // teacher's places' logits, which may lie where it is written.)
+        auto exchange = [&](int p, int r, float m, float s) {
+            tc::mbar_wait(&tfull[p], r >> 1 & 1, abort, &g_err_distill, 1u);
+            if (threadIdx.x < ranks) {
+                cluster_store(&all_m[p][rank], threadIdx.x, m);
+                cluster_store(&all_s[p][rank], threadIdx.x, s);
+                cluster_arrive(&got[p], threadIdx.x);
+            }
+            cluster_wait(&got[p], r >> 1 & 1, abort);
+        };
+        for (int r = 0; r < mine; ++r) {
+            const int p = r & 1;
+            const int64_t row = first + (int64_t)r * clusters;
+            const T* z = Z + row * a.ldz;
+            const uint32_t head = head_of(z);
+            const int nvec = (len - head) / N;
+            edge = edge_at_next;
+            edge_z = edge_next;
+            edge_at_next = edge_of(r + 1, &edge_next);
+            const int slot0 = slot;
+            float L;
+            if (sums) {
+                Running run;
+                for (int o = 0; o < nvec; o += 2 * THREADS) {
+                    tc::mbar_wait(&full[slot], phase, abort, &g_err_distill, 1u);
+                    const uint4* v = reinterpret_cast<const uint4*>(ring + slot * kChunk);
+                    float x[2][N];
 #pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-        const int64_t k = threadIdx.x + u * kThreads;
-        mine[u] = 0.f;
-        if (c != 0.f && k < a.K && at[k] >= 0) {
-            float sum = 0.f;
-            for (int64_t o = 0; o < a.K; ++o)
-                if (at[o] == at[k]) sum += p[o];
-            mine[u] = c * (expf(el::to_f32(z[at[k]]) * it - L) - sum);
-        }
-    }
-    __syncthreads();
-    for (int64_t j = threadIdx.x; j < a.V; j += kThreads)
-        d[j] = el::from_f32<T>(c != 0.f ? c * expf(el::to_f32(z[j]) * it - L) : 0.f);
-    __syncthreads();
-    if (c != 0.f) {
+                    for (int u = 0; u < 2; ++u) {
+                        if (o + u * THREADS + (int)threadIdx.x < nvec) {
+                            widen(v[u * THREADS + threadIdx.x], x[u], T());
+                        } else {
 #pragma unroll
-        for (int u = 0; u < kEach; ++u) {
-            const int64_t k = threadIdx.x + u * kThreads;
-            if (k < a.K && at[k] >= 0) d[at[k]] = el::from_f32<T>(mine[u]);
+                            for (int e = 0; e < N; ++e) x[u][e] = -INFINITY;
+                        }
+                    }
+                    if (!(dZ && a.keep)) {
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive(&empty[slot]);
+                    }
+                    if (++slot == a.chunks) {
+                        slot = 0;
+                        phase ^= 1;
+                    }
+                    float top = x[0][0];
+#pragma unroll
+                    for (int e = 1; e < 2 * N; ++e) top = max_nan(top, x[e / N][e % N]);
+                    run.raise(top, k2);
+                    float s[4] = {};
+#pragma unroll
+                    for (int e = 0; e < 2 * N; ++e) s[e & 3] += ex2(fmaf(x[e / N][e % N], k2, run.shift));
+                    run.s += (s[0] + s[1]) + (s[2] + s[3]);
+                }
+                if (edge >= 0) {
+                    run.raise(edge_z, k2);
+                    run.s += ex2(fmaf(edge_z, k2, run.shift));
+                }
+                float m = run.m;
+#pragma unroll
+                for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+                float s = el::warp_sum(run.m == m ? run.s : run.s * ex2((run.m - m) * k2));
+                if (lane == 0) part_m[p][warp] = m, part_s[p][warp] = s;
+                tc::named_bar_sync(1, THREADS);
+                Running all;
+#pragma unroll
+                for (int i = 0; i < kWarps; ++i) all.m = max_nan(all.m, part_m[p][i]);
+#pragma unroll
+                for (int i = 0; i < kWarps; ++i) {
+                    const float pm = part_m[p][i];
+                    all.s += pm == all.m ? part_s[p][i] : part_s[p][i] * ex2((pm - all.m) * k2);
+                }
+                if (ranks > 1) {
+                    exchange(p, r, all.m, all.s);
+                    Running both;
+                    for (uint32_t i = 0; i < ranks; ++i) both.join(all_m[p][i], all_s[p][i], k2);
+                    all = both;
+                }
+                L = fmaf(all.m, it, logf(all.s));
+                if (a.lse_out && rank == 0 && threadIdx.x == 0) a.lse_out[row] = L;
+            } else {
+                if (ranks > 1) exchange(p, r, 0.f, 0.f);
+                L = __ldg(a.lse_in + row);
+            }
+            tc::mbar_wait(&tfull[p], r >> 1 & 1, abort, &g_err_distill, 1u);
+            const float c = teacher[p].c, shift = -L * kLog2e;
+            const int* my_at = at + p * a.K;
+            const float *my_p = pk + p * a.K, *my_lp = lpk + p * a.K, *my_z = zk + p * a.K;
+            if (a.loss && rank == 0 && warp == 0) {
+                float kl = 0.f;
+                for (int k = lane; k < a.K; k += 32)
+                    if (my_p[k] != 0.f) kl = fmaf(my_p[k], my_lp[k] - fmaf(my_z[k], it, -L), kl);
+                kl = el::warp_sum(kl);
+                const float lw = teacher[p].lw;
+                if (lane == 0) a.loss[row] = lw != 0.f ? lw * kl : 0.f;
+            }
+            if (dZ) {
+                T* d = dZ + row * a.lddz;
+                const bool same = ((reinterpret_cast<uintptr_t>(d) ^ reinterpret_cast<uintptr_t>(z)) & 15u) == 0;
+                const bool again = sums && a.keep;            // the chunks of the sum, still there
+                int at_slot = again ? slot0 : slot;
+                for (int o = 0; o < nvec; o += 2 * THREADS) {
+                    if (!again) tc::mbar_wait(&full[at_slot], phase, abort, &g_err_distill, 1u);
+                    uint4* v = reinterpret_cast<uint4*>(ring + at_slot * kChunk);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int i = o + u * THREADS + threadIdx.x;
+                        if (i < nvec) {
+                            float x[N];
+                            uint4 out = make_uint4(0, 0, 0, 0);
+                            if (c != 0.f) {
+                                widen(v[u * THREADS + threadIdx.x], x, T());
+#pragma unroll
+                                for (int e = 0; e < N; ++e) x[e] = c * ex2(fmaf(x[e], k2, shift));
+                                out = narrow(x, T());
+                            }
+                            if (same) *reinterpret_cast<uint4*>(d + head + (int64_t)i * N) = out;
+                            else v[u * THREADS + threadIdx.x] = out;
+                        }
+                    }
+                    if (!same) {
+                        // a warp's vectors side by side, element by element
+                        __syncwarp();
+                        const T* from = reinterpret_cast<const T*>(v);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int v0 = u * THREADS + warp * 32;
+                            const int n = min(nvec - (o + v0), 32) * N;
+#pragma unroll 4
+                            for (int e = lane; e < n; e += 32) d[head + (int64_t)(o + v0) * N + e] = from[v0 * N + e];
+                        }
+                        tc::fence_proxy_async_smem();         // the place's next copy comes after these writes
+                    }
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(&empty[at_slot]);
+                    if (++at_slot == a.chunks) {
+                        at_slot = 0;
+                        if (!again) phase ^= 1;
+                    }
+                }
+                if (!again) slot = at_slot;
+                if (edge >= 0) d[edge] = el::from_f32<T>(c != 0.f ? c * ex2(fmaf(edge_z, k2, shift)) : 0.f);
+                tc::named_bar_sync(1, THREADS);
+                if (c != 0.f) {
+                    for (int k = threadIdx.x; k < a.K; k += THREADS) {
+                        const int64_t i = (int64_t)my_at[k] - c0;
+                        if (my_at[k] < 0 || i < 0 || i >= len) continue;
+                        float sum = my_p[k];
+                        if (teacher[p].repeated) {
+                            sum = 0.f;
+                            for (int o = 0; o < a.K; ++o)
+                                if (my_at[o] == my_at[k]) sum += my_p[o];
+                        }
+                        d[i] = el::from_f32<T>(c * (ex2(fmaf(my_z[k], k2, shift)) - sum));
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&tempty[p]);
         }
     }
+    if (ranks > 1) cluster_sync();           // no block ends before the others have given it theirs
+}
+
+constexpr int kSmem = 216 * 1024;            // of a multiprocessor, for rings and teacher entries
+
+template <typename T, int THREADS>
+lrc_status distill_launch(Args a, int ranks, int resident, cudaStream_t s) {
+    constexpr int kChunk = THREADS * 32;
+    const int extra = 8 * 4 * a.K + 4 * a.table;
+    int room = kSmem / resident - extra - (resident > 1 ? 2048 : 0);
+    a.chunks = room / kChunk < kMostChunks ? room / kChunk : kMostChunks;
+    const int64_t need = (a.slice * (int64_t)sizeof(T) + kChunk - 1) / kChunk;
+    a.keep = need <= a.chunks;
+    const int smem = a.chunks * kChunk + extra;
+    auto kernel = distill_kernel<T, THREADS>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return cuda_fail(e, "distill_kernel");
+    int64_t clusters = (int64_t)sm_count() * resident / ranks;
+    if (clusters > a.rows) clusters = a.rows;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(clusters * ranks));
+    cfg.blockDim = dim3(THREADS + 64);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)ranks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = ranks > 1 ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, kernel, a);
+    if (e != cudaSuccess) return cuda_fail(e, "distill_kernel");
+    return after_launch("distill_kernel");
+}
+
+template <typename T>
+lrc_status distill_as(Args a, cudaStream_t s) {
+    // Few rows: a cluster of up to eight blocks each, of 4096 elements at least.
+    int ranks = 1;
+    while (ranks < 8 && a.rows * ranks * 2 <= sm_count() && a.V >= ranks * 2 * 4096) ranks *= 2;
+    a.slice = ((a.V + ranks - 1) / ranks + 7) / 8 * 8;
+    // Short rows: several small blocks on a multiprocessor, whose rows' chains overlap.
+    const int64_t bytes = a.slice * (int64_t)sizeof(T);
+    if (bytes > 49152) return distill_launch<T, 512>(a, ranks, 1, s);
+    if (bytes > 16384) return distill_launch<T, 256>(a, ranks, 2, s);
+    return distill_launch<T, 128>(a, ranks, 4, s);
 }
 
 }  // namespace
@@ -129,14 +540,41 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(Args a) {
 lrc_status launch_distill(const void* Z, const void* T, const int64_t* idx, const float* w, const float* lse_in,
                           const float* g, float* loss, float* lse_out, void* dZ, int64_t rows, int64_t V, int64_t K,
                           int64_t ldz, int64_t ldt, int64_t lddz, float tau, lrc_fmt fmt, lrc_fmt tfmt, cudaStream_t s) {
-    Args a{Z, T, idx, w, lse_in, g, loss, lse_out, dZ, V, K, ldz, ldt, lddz, tau,
-           tfmt == LRC_F32 ? 0 : tfmt == LRC_BF16 ? 2 : 1};
-    if (fmt == LRC_F32) distill_kernel<float><<<(unsigned)rows, kThreads, 0, s>>>(a);
-    else if (fmt == LRC_BF16) distill_kernel<bf16><<<(unsigned)rows, kThreads, 0, s>>>(a);
-    else distill_kernel<__half><<<(unsigned)rows, kThreads, 0, s>>>(a);
-    return after_launch("distill_kernel");
+    Args a{};
+    a.Z = Z;
+    a.T = T;
+    a.idx = idx;
+    a.w = w;
+    a.lse_in = lse_in;
+    a.g = g;
+    a.loss = loss;
+    a.lse_out = lse_out;
+    a.dZ = dZ;
+    a.rows = rows;
+    a.V = V;
+    a.ldz = ldz;
+    a.ldt = ldt;
+    a.lddz = lddz;
+    a.K = (int)K;
+    a.table = 64;
+    while (a.table < 2 * K) a.table *= 2;
+    a.tau = tau;
+    a.tkind = tfmt == LRC_F32 ? 0 : tfmt == LRC_BF16 ? 2 : 1;
+    if (fmt == LRC_F32) return distill_as<float>(a, s);
+    if (fmt == LRC_BF16) return distill_as<bf16>(a, s);
+    return distill_as<__half>(a, s);
 }
 
 int distill_max_top() { return kMaxTop; }
+
+uint32_t take_distill_error() {
+    unsigned int v = 0;
+    if (cudaMemcpyFromSymbol(&v, g_err_distill, sizeof v) != cudaSuccess) return 0xffffffffu;
+    if (v) {
+        const unsigned int z = 0;
+        cudaMemcpyToSymbol(g_err_distill, &z, sizeof z);
+    }
+    return v;
+}
 
 }  // namespace lrc
