@@ -11,7 +11,8 @@
 //
 // Persistent blocks, one row at a time (or a cluster a row where rows are few, each
 // block a slice).  One warp brings the row in chunks by bulk copies into a ring in
-// shared memory, another one prepares the next row's teacher entries, the others
+// shared memory, a few prepare the next rows' teacher entries (a row each: a chain of
+// two loads from memory and a softmax, longer than many a row's copies), the others
 // form the running maximum and sum chunk by chunk as they come and, where the row
 // fits into the ring, the gradient from the same copy; else the chunks come again
 // (from L2).  The ring holds the next row's first chunks by then.  At the places of
@@ -161,22 +162,25 @@ struct Teacher {
     int repeated;            // some place is named more than once
 };
 
-// Shared memory: ring | per row parity: at, p, log p, z of the K entries | table.
+// Warps that prepare teacher entries: one for each row that is prepared ahead.
+constexpr int teachers(int THREADS) { return THREADS > 256 ? 4 : 2; }
+constexpr int all_threads(int THREADS) { return THREADS + 32 + 32 * teachers(THREADS); }
+
+// Shared memory: ring | a teacher's warp each: at, log p, z of the K entries, table.
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS + 64, 512 / THREADS) distill_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_kernel(const __grid_constant__ Args a) {
     constexpr int kChunk = THREADS * 32;                      // bytes: two vectors a thread
-    constexpr int kWarps = THREADS / 32, N = kVec<T>;
+    constexpr int kWarps = THREADS / 32, N = kVec<T>, kAhead = teachers(THREADS);
     extern __shared__ __align__(128) uint8_t ring[];
-    __shared__ uint64_t full[kMostChunks], empty[kMostChunks], tfull[2], tempty[2], got[2];
+    __shared__ uint64_t full[kMostChunks], empty[kMostChunks], tfull[kAhead], tempty[kAhead], got[2];
     __shared__ float part_m[2][kWarps], part_s[2][kWarps];    // [row parity][warp]
     __shared__ float all_m[2][8], all_s[2][8];                // [row parity][block of the cluster]
-    __shared__ Teacher teacher[2];
+    __shared__ Teacher teacher[kAhead];
     __shared__ int abort_flag;
-    int* at = reinterpret_cast<int*>(ring + a.chunks * kChunk);          // [2][K]
-    float* pk = reinterpret_cast<float*>(at + 2 * a.K);
-    float* lpk = pk + 2 * a.K;
-    float* zk = lpk + 2 * a.K;
-    int* table = reinterpret_cast<int*>(zk + 2 * a.K);
+    int* at = reinterpret_cast<int*>(ring + a.chunks * kChunk);          // [kAhead][K]
+    float* lpk = reinterpret_cast<float*>(at + kAhead * a.K);
+    float* zk = lpk + kAhead * a.K;
+    int* tables = reinterpret_cast<int*>(zk + kAhead * a.K);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t ranks = cluster_size(), rank = cluster_rank();
@@ -195,11 +199,11 @@ __global__ void __launch_bounds__(THREADS + 64, 512 / THREADS) distill_kernel(co
             tc::mbar_init(&full[d], 1);
             tc::mbar_init(&empty[d], kWarps);
         }
-        for (int p = 0; p < 2; ++p) {
+        for (int p = 0; p < kAhead; ++p) {
             tc::mbar_init(&tfull[p], 1);
             tc::mbar_init(&tempty[p], kWarps);
-            tc::mbar_init(&got[p], ranks);
         }
+        for (int p = 0; p < 2; ++p) tc::mbar_init(&got[p], ranks);
         tc::fence_barrier_init();
     }
     if (ranks > 1) cluster_sync();                            // every block's barriers are there
@@ -245,19 +249,22 @@ __global__ void __launch_bounds__(THREADS + 64, 512 / THREADS) distill_kernel(co
                 tc::mbar_wait(&full[u % a.chunks], u / a.chunks & 1, &no_abort, &g_err_distill, 1u);
         }
         __syncwarp();
-    } else if (warp == kWarps + 1) {
-        // ---- the teacher's entries, a row ahead
+    } else if (warp > kWarps) {
+        // ---- the teacher's entries, rows ahead
         const float none = -INFINITY;
-        for (int r = 0; r < mine; ++r) {
-            const int p = r & 1;
-            if (r >= 2) tc::mbar_wait(&tempty[p], (r >> 1 & 1) ^ 1, abort, &g_err_distill, 1u);
+        const int p = warp - kWarps - 1;
+        int* table = tables + p * a.table;
+        uint32_t phase = 1;
+        for (int r = p; r < mine; r += kAhead) {
+            if (r >= kAhead) tc::mbar_wait(&tempty[p], phase, abort, &g_err_distill, 1u);
+            phase ^= 1;
             __syncwarp();
             const int64_t row = first + (int64_t)r * clusters;
             const T* z = static_cast<const T*>(a.Z) + row * a.ldz;
             int* my_at = at + p * a.K;
-            float *my_p = pk + p * a.K, *my_lp = lpk + p * a.K, *my_z = zk + p * a.K;
+            float *my_lp = lpk + p * a.K, *my_z = zk + p * a.K;
             float top = none;
-#pragma unroll 2
+#pragma unroll 4
             for (int k = lane; k < a.K; k += 32) {
                 const int64_t i = __ldg(a.idx + row * a.ldt + k);
                 const bool there = i >= 0 && i < a.V;
@@ -265,7 +272,7 @@ __global__ void __launch_bounds__(THREADS + 64, 512 / THREADS) distill_kernel(co
                 const bool in = t != none;                    // (a NaN is)
                 my_at[k] = in ? (int)i : -1;
                 my_z[k] = in ? el::to_f32(z[i]) : 0.f;
-                my_p[k] = t;
+                my_lp[k] = t;
                 top = max_nan(top, t);
             }
             const float w = a.w ? __ldg(a.w + row) : 1.f, g = a.g ? __ldg(a.g + row) : 1.f;
@@ -273,16 +280,14 @@ __global__ void __launch_bounds__(THREADS + 64, 512 / THREADS) distill_kernel(co
 #pragma unroll
             for (int o = 16; o; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
             float s = 0.f;
-            for (int k = lane; k < a.K; k += 32) s += expf(my_p[k] - top);
+            for (int k = lane; k < a.K; k += 32) s += expf(my_lp[k] - top);
             s = el::warp_sum(s);
             const float lt = top + logf(s);
             int repeated = 0;
             __syncwarp();
             for (int k = lane; k < a.K; k += 32) {
                 const int i = my_at[k];
-                const float lp = my_p[k] - lt;
-                my_lp[k] = lp;
-                my_p[k] = i < 0 ? 0.f : expf(lp);
+                my_lp[k] = i < 0 ? none : my_lp[k] - lt;
                 if (i >= 0) {
                     uint32_t h = (uint32_t)i * 2654435761u >> 16;
                     while (true) {                            // (the table has twice as many places)
@@ -327,7 +332,6 @@ __global__ void __launch_bounds__(THREADS + 64, 512 / THREADS) distill_kernel(co
         // had read those of row r.  And no block writes a gradient before all have their
         // teacher's places' logits, which may lie where it is written.)
         auto exchange = [&](int p, int r, float m, float s) {
-            tc::mbar_wait(&tfull[p], r >> 1 & 1, abort, &g_err_distill, 1u);
             if (threadIdx.x < ranks) {
                 cluster_store(&all_m[p][rank], threadIdx.x, m);
                 cluster_store(&all_s[p][rank], threadIdx.x, s);
@@ -335,8 +339,12 @@ __global__ void __launch_bounds__(THREADS + 64, 512 / THREADS) distill_kernel(co
             }
             cluster_wait(&got[p], r >> 1 & 1, abort);
         };
+        int ahead = -1;                      // the row's teacher entries
+        uint32_t tphase = 1;
         for (int r = 0; r < mine; ++r) {
             const int p = r & 1;
+            if (++ahead == kAhead) ahead = 0;
+            if (ahead == 0) tphase ^= 1;
             const int64_t row = first + (int64_t)r * clusters;
             const T* z = Z + row * a.ldz;
             const uint32_t head = head_of(z);
@@ -397,6 +405,7 @@ __global__ void __launch_bounds__(THREADS + 64, 512 / THREADS) distill_kernel(co
                     all.s += pm == all.m ? part_s[p][i] : part_s[p][i] * ex2((pm - all.m) * k2);
                 }
                 if (ranks > 1) {
+                    tc::mbar_wait(&tfull[ahead], tphase, abort, &g_err_distill, 1u);
                     exchange(p, r, all.m, all.s);
                     Running both;
                     for (uint32_t i = 0; i < ranks; ++i) both.join(all_m[p][i], all_s[p][i], k2);
@@ -405,19 +414,24 @@ __global__ void __launch_bounds__(THREADS + 64, 512 / THREADS) distill_kernel(co
                 L = fmaf(all.m, it, logf(all.s));
                 if (a.lse_out && rank == 0 && threadIdx.x == 0) a.lse_out[row] = L;
             } else {
-                if (ranks > 1) exchange(p, r, 0.f, 0.f);
+                if (ranks > 1) {
+                    tc::mbar_wait(&tfull[ahead], tphase, abort, &g_err_distill, 1u);
+                    exchange(p, r, 0.f, 0.f);
+                }
                 L = __ldg(a.lse_in + row);
             }
-            tc::mbar_wait(&tfull[p], r >> 1 & 1, abort, &g_err_distill, 1u);
-            const float c = teacher[p].c, shift = -L * kLog2e;
-            const int* my_at = at + p * a.K;
-            const float *my_p = pk + p * a.K, *my_lp = lpk + p * a.K, *my_z = zk + p * a.K;
+            tc::mbar_wait(&tfull[ahead], tphase, abort, &g_err_distill, 1u);
+            const float c = teacher[ahead].c, shift = -L * kLog2e;
+            const int* my_at = at + ahead * a.K;
+            const float *my_lp = lpk + ahead * a.K, *my_z = zk + ahead * a.K;
             if (a.loss && rank == 0 && warp == 0) {
                 float kl = 0.f;
-                for (int k = lane; k < a.K; k += 32)
-                    if (my_p[k] != 0.f) kl = fmaf(my_p[k], my_lp[k] - fmaf(my_z[k], it, -L), kl);
+                for (int k = lane; k < a.K; k += 32) {
+                    const float pk = expf(my_lp[k]);
+                    if (pk != 0.f) kl = fmaf(pk, my_lp[k] - fmaf(my_z[k], it, -L), kl);
+                }
                 kl = el::warp_sum(kl);
-                const float lw = teacher[p].lw;
+                const float lw = teacher[ahead].lw;
                 if (lane == 0) a.loss[row] = lw != 0.f ? lw * kl : 0.f;
             }
             if (dZ) {
@@ -471,18 +485,18 @@ __global__ void __launch_bounds__(THREADS + 64, 512 / THREADS) distill_kernel(co
                     for (int k = threadIdx.x; k < a.K; k += THREADS) {
                         const int64_t i = (int64_t)my_at[k] - c0;
                         if (my_at[k] < 0 || i < 0 || i >= len) continue;
-                        float sum = my_p[k];
-                        if (teacher[p].repeated) {
+                        float sum = expf(my_lp[k]);
+                        if (teacher[ahead].repeated) {
                             sum = 0.f;
                             for (int o = 0; o < a.K; ++o)
-                                if (my_at[o] == my_at[k]) sum += my_p[o];
+                                if (my_at[o] == my_at[k]) sum += expf(my_lp[o]);
                         }
                         d[i] = el::from_f32<T>(c * (ex2(fmaf(my_z[k], k2, shift)) - sum));
                     }
                 }
             }
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&tempty[p]);
+            if (lane == 0) tc::mbar_arrive(&tempty[ahead]);
         }
     }
     if (ranks > 1) cluster_sync();           // no block ends before the others have given it theirs
@@ -493,7 +507,7 @@ constexpr int kSmem = 216 * 1024;            // of a multiprocessor, for rings a
 template <typename T, int THREADS>
 lrc_status distill_launch(Args a, int ranks, int resident, cudaStream_t s) {
     constexpr int kChunk = THREADS * 32;
-    const int extra = 8 * 4 * a.K + 4 * a.table;
+    const int extra = teachers(THREADS) * 4 * (3 * a.K + a.table);
     int room = kSmem / resident - extra - (resident > 1 ? 2048 : 0);
     a.chunks = room / kChunk < kMostChunks ? room / kChunk : kMostChunks;
     const int64_t need = (a.slice * (int64_t)sizeof(T) + kChunk - 1) / kChunk;
@@ -506,7 +520,7 @@ lrc_status distill_launch(Args a, int ranks, int resident, cudaStream_t s) {
     if (clusters > a.rows) clusters = a.rows;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(clusters * ranks));
-    cfg.blockDim = dim3(THREADS + 64);
+    cfg.blockDim = dim3(all_threads(THREADS));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -525,13 +539,18 @@ lrc_status distill_launch(Args a, int ranks, int resident, cudaStream_t s) {
 template <typename T>
 lrc_status distill_as(Args a, cudaStream_t s) {
     // Few rows: a cluster of up to eight blocks each, of 4096 elements at least.
+    // (Clusters for rows that no block can keep are slower than reading them twice, the
+    // second time from L2: 215 us against 133 for 512 rows of 262144 bfloat16.)
     int ranks = 1;
     while (ranks < 8 && a.rows * ranks * 2 <= sm_count() && a.V >= ranks * 2 * 4096) ranks *= 2;
     a.slice = ((a.V + ranks - 1) / ranks + 7) / 8 * 8;
-    // Short rows: several small blocks on a multiprocessor, whose rows' chains overlap.
+    // Rows of up to 16 KB: four small blocks on a multiprocessor, whose rows' chains
+    // overlap (4096 rows of 8192 binary16: 37 us, with two 44 us); up to 98 KB: two
+    // where the sum is formed (2048 rows of 32768 bfloat16: 58 us, with one 69 us), one
+    // for the gradient alone (1021 x 50001 binary16: 36 us, with two 40 us).
     const int64_t bytes = a.slice * (int64_t)sizeof(T);
-    if (bytes > 49152) return distill_launch<T, 512>(a, ranks, 1, s);
-    if (bytes > 16384) return distill_launch<T, 256>(a, ranks, 2, s);
+    if (bytes > (a.lse_in ? 48 : 98) * 1024) return distill_launch<T, 512>(a, ranks, 1, s);
+    if (bytes > 16 * 1024) return distill_launch<T, 256>(a, ranks, 2, s);
     return distill_launch<T, 128>(a, ranks, 4, s);
 }
 
