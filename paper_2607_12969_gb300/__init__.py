@@ -138,6 +138,17 @@ def _fmt(fmt) -> int:
     return int(fmt)
 
 
+# format (name or code) -> code, element types of storage and output
+_TYPES = {}
+
+
+def _types(fmt):
+    known = _TYPES.get(fmt)
+    if known is None:
+        known = _TYPES[fmt] = (_fmt(fmt), storage_dtype(fmt), output_dtype(fmt))
+    return known
+
+
 def storage_dtype(fmt):
     _T()
     f = _fmt(fmt)
@@ -516,9 +527,27 @@ def lrc_selftest_wait_timeout(limit_ns: int, stream=None) -> None:
 # the operators around a compressed layer
 # --------------------------------------------------------------------------
 
-def _check_optional(t, what: str, dtype, elems: int, dev: int, stream) -> None:
-    if t is not None:
-        _check_arg(t, what, dtype, elems, dev, stream)
+def _addr(t, what: str, dtype, elems: int, dev: int, stream) -> int:
+    """Address of t after _check_arg's checks: for a contiguous tensor on the
+    call's GPU by its element count, which costs a third of them."""
+    try:
+        if t.get_device() == dev and t.dtype is dtype and t.is_contiguous() and t.numel() >= elems:
+            return t.data_ptr()
+    except AttributeError:          # no tensor: the checks by name say so
+        pass
+    _check_arg(t, what, dtype, elems, dev, stream)
+    return t.data_ptr()
+
+
+def _addr_or_none(t, what: str, dtype, elems: int, dev: int, stream) -> int:
+    return 0 if t is None else _addr(t, what, dtype, elems, dev, stream)
+
+
+def _handle(stream, dev: int) -> int:
+    """The stream's handle, of the current stream of GPU dev for None."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(dev)
+    return _stream(stream)
 
 
 def lrc_q4_row_bytes(n: int) -> int:
@@ -526,114 +555,114 @@ def lrc_q4_row_bytes(n: int) -> int:
     return int(load().lrc_q4_row_bytes(int(n)))
 
 
-def _check_q4(Q, scales, zeros, m, n, group, f, dev, stream) -> None:
-    st, torch = storage_dtype(f), _T()
-    if m > 0 and n > 0 and group > 0:
-        span = ((n + group - 1) // group - 1) * ((m + 15) // 16 * 16) + m
-        _check_arg(Q, "Q", torch.uint8, m * ((n + 127) // 128 * 64), dev, stream)
-        _check_arg(scales, "scales", st, span, dev, stream)
-        _check_optional(zeros, "zeros", torch.uint8, span, dev, stream)
+def _q4_addrs(Q, scales, zeros, m, n, group, st, dev, stream):
+    if not (m > 0 and n > 0 and group > 0):      # left to the library's validation
+        return _ptr(Q), _ptr(scales), _ptr(zeros)
+    u8 = _T().uint8
+    span = ((n + group - 1) // group - 1) * ((m + 15) // 16 * 16) + m
+    return (_addr(Q, "Q", u8, m * ((n + 127) // 128 * 64), dev, stream),
+            _addr(scales, "scales", st, span, dev, stream),
+            _addr_or_none(zeros, "zeros", u8, span, dev, stream))
 
 
 def lrc_q4_round(W, wfmt, m: int, n: int, ldw: int, Q, scales, zeros, group: int, fmt, stream=None):
     """Rounds W to 4-bit codes Q with scales (and zero codes, or None)."""
-    f, fw, dev = _fmt(fmt), _fmt(wfmt), _call_device(stream)
-    _check_arg(W, "W", storage_dtype(fw), _extent(m, n, ldw), dev, stream)
-    _check_q4(Q, scales, zeros, m, n, group, f, dev, stream)
-    _check(load().lrc_q4_round(_ptr(W), fw, m, n, ldw, _ptr(Q), _ptr(scales), _ptr(zeros), group, f, _stream(stream)))
+    (f, st, _), (fw, wt, _), dev = _types(fmt), _types(wfmt), _call_device(stream)
+    w = _addr(W, "W", wt, _extent(m, n, ldw), dev, stream)
+    q, s, z = _q4_addrs(Q, scales, zeros, m, n, group, st, dev, stream)
+    _check(load().lrc_q4_round(w, fw, m, n, ldw, q, s, z, group, f, _handle(stream, dev)))
 
 
 def lrc_q4_widen(Q, scales, zeros, group: int, fmt, m: int, n: int, dst, dfmt, ld_dst: int, stream=None):
     """The values a 4-bit matrix stands for, in format dfmt's storage type."""
-    f, fd, dev = _fmt(fmt), _fmt(dfmt), _call_device(stream)
-    _check_q4(Q, scales, zeros, m, n, group, f, dev, stream)
-    _check_arg(dst, "dst", storage_dtype(fd), _extent(m, n, ld_dst), dev, stream)
-    _check(load().lrc_q4_widen(_ptr(Q), _ptr(scales), _ptr(zeros), group, f, m, n, _ptr(dst), fd, ld_dst,
-                               _stream(stream)))
+    (f, st, _), (fd, dt, _), dev = _types(fmt), _types(dfmt), _call_device(stream)
+    q, s, z = _q4_addrs(Q, scales, zeros, m, n, group, st, dev, stream)
+    d = _addr(dst, "dst", dt, _extent(m, n, ld_dst), dev, stream)
+    _check(load().lrc_q4_widen(q, s, z, group, f, m, n, d, fd, ld_dst, _handle(stream, dev)))
 
 
 def lrc_q4_apply(Q, scales, zeros, X, A, Y, m: int, n: int, b: int, group: int, fmt, stream=None):
     """Y = A + X What^T for a 4-bit matrix What and b vectors; A may be None or Y."""
-    f, dev = _fmt(fmt), _call_device(stream)
-    _check_q4(Q, scales, zeros, m, n, group, f, dev, stream)
+    (f, st, out), dev = _types(fmt), _call_device(stream)
+    q, s, z = _q4_addrs(Q, scales, zeros, m, n, group, st, dev, stream)
     if m > 0 and n > 0 and b > 0:
-        out = output_dtype(f)
-        _check_arg(X, "X", storage_dtype(f), (b - 1) * ((n + 15) // 16 * 16) + n, dev, stream)
-        _check_optional(A, "A", out, b * m, dev, stream)
-        _check_arg(Y, "Y", out, b * m, dev, stream)
-    _check(load().lrc_q4_apply(_ptr(Q), _ptr(scales), _ptr(zeros), _ptr(X), _ptr(A), _ptr(Y), m, n, b, group, f,
-                               _stream(stream)))
+        x = _addr(X, "X", st, (b - 1) * ((n + 15) // 16 * 16) + n, dev, stream)
+        a = _addr_or_none(A, "A", out, b * m, dev, stream)
+        y = _addr(Y, "Y", out, b * m, dev, stream)
+    else:
+        x, a, y = _ptr(X), _ptr(A), _ptr(Y)
+    _check(load().lrc_q4_apply(q, s, z, x, a, y, m, n, b, group, f, _handle(stream, dev)))
 
 
 def lrc_layer_norm(X, gamma, beta, Y, mean, rstd, rows: int, cols: int, ldx: int, ldy: int, eps: float, fmt, pfmt,
                    stream=None):
     """Layer norm of the rows of X into Y; gamma, beta, mean and rstd may be None."""
-    f, fp, dev = _fmt(fmt), _fmt(pfmt), _call_device(stream)
-    st, out, pt, f32 = storage_dtype(f), output_dtype(f), storage_dtype(fp), _T().float32
+    (f, st, out), (fp, pt, _), dev, f32 = _types(fmt), _types(pfmt), _call_device(stream), _T().float32
     if rows > 0 and cols > 0:
-        _check_arg(X, "X", st, (rows - 1) * ldx + cols, dev, stream)
-        _check_optional(gamma, "gamma", pt, cols, dev, stream)
-        _check_optional(beta, "beta", pt, cols, dev, stream)
-        _check_arg(Y, "Y", out, (rows - 1) * ldy + cols, dev, stream)
-        _check_optional(mean, "mean", f32, rows, dev, stream)
-        _check_optional(rstd, "rstd", f32, rows, dev, stream)
-    _check(load().lrc_layer_norm(_ptr(X), _ptr(gamma), _ptr(beta), _ptr(Y), _ptr(mean), _ptr(rstd), rows, cols, ldx, ldy,
-                                 float(eps), f, fp, _stream(stream)))
+        x = _addr(X, "X", st, (rows - 1) * ldx + cols, dev, stream)
+        g = _addr_or_none(gamma, "gamma", pt, cols, dev, stream)
+        b = _addr_or_none(beta, "beta", pt, cols, dev, stream)
+        y = _addr(Y, "Y", out, (rows - 1) * ldy + cols, dev, stream)
+        mu = _addr_or_none(mean, "mean", f32, rows, dev, stream)
+        r = _addr_or_none(rstd, "rstd", f32, rows, dev, stream)
+    else:
+        x, g, b, y, mu, r = _ptr(X), _ptr(gamma), _ptr(beta), _ptr(Y), _ptr(mean), _ptr(rstd)
+    _check(load().lrc_layer_norm(x, g, b, y, mu, r, rows, cols, ldx, ldy, eps, f, fp, _handle(stream, dev)))
 
 
 def lrc_layer_norm_grad(dY, X, gamma, mean, rstd, dX, dgamma, dbeta, rows: int, cols: int, lddy: int, ldx: int,
                         lddx: int, fmt, pfmt, stream=None):
     """Gradient of lrc_layer_norm; gamma, dX, dgamma and dbeta may be None."""
-    f, fp, dev = _fmt(fmt), _fmt(pfmt), _call_device(stream)
-    st, out, pt, f32 = storage_dtype(f), output_dtype(f), storage_dtype(fp), _T().float32
+    (f, st, out), (fp, pt, _), dev, f32 = _types(fmt), _types(pfmt), _call_device(stream), _T().float32
     if rows > 0 and cols > 0:
-        _check_arg(dY, "dY", out, (rows - 1) * lddy + cols, dev, stream)
-        _check_arg(X, "X", st, (rows - 1) * ldx + cols, dev, stream)
-        _check_optional(gamma, "gamma", pt, cols, dev, stream)
-        _check_arg(mean, "mean", f32, rows, dev, stream)
-        _check_arg(rstd, "rstd", f32, rows, dev, stream)
-        _check_optional(dX, "dX", st, (rows - 1) * lddx + cols, dev, stream)
-    _check_optional(dgamma, "dgamma", f32, cols, dev, stream)
-    _check_optional(dbeta, "dbeta", f32, cols, dev, stream)
-    _check(load().lrc_layer_norm_grad(_ptr(dY), _ptr(X), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dX), _ptr(dgamma),
-                                      _ptr(dbeta), rows, cols, lddy, ldx, lddx, f, fp, _stream(stream)))
+        dy = _addr(dY, "dY", out, (rows - 1) * lddy + cols, dev, stream)
+        x = _addr(X, "X", st, (rows - 1) * ldx + cols, dev, stream)
+        g = _addr_or_none(gamma, "gamma", pt, cols, dev, stream)
+        mu = _addr(mean, "mean", f32, rows, dev, stream)
+        r = _addr(rstd, "rstd", f32, rows, dev, stream)
+        dx = _addr_or_none(dX, "dX", st, (rows - 1) * lddx + cols, dev, stream)
+    else:
+        dy, x, g, mu, r, dx = _ptr(dY), _ptr(X), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dX)
+    dg = _addr_or_none(dgamma, "dgamma", f32, cols, dev, stream)
+    db = _addr_or_none(dbeta, "dbeta", f32, cols, dev, stream)
+    _check(load().lrc_layer_norm_grad(dy, x, g, mu, r, dx, dg, db, rows, cols, lddy, ldx, lddx, f, fp,
+                                      _handle(stream, dev)))
 
 
-def _check_distill(Z, T, idx, w, dZ, rows, V, K, ldz, ldt, lddz, f, ft, dev, stream) -> None:
-    st, tt, torch = storage_dtype(f), storage_dtype(ft), _T()
-    if rows > 0 and V > 0 and K > 0:
-        _check_arg(Z, "Z", st, (rows - 1) * ldz + V, dev, stream)
-        _check_arg(T, "T", tt, (rows - 1) * ldt + K, dev, stream)
-        _check_arg(idx, "idx", torch.int64, (rows - 1) * ldt + K, dev, stream)
-        _check_optional(w, "w", torch.float32, rows, dev, stream)
-        _check_optional(dZ, "dZ", st, (rows - 1) * lddz + V, dev, stream)
+def _distill_addrs(Z, T, idx, w, rows, V, K, ldz, ldt, st, tt, dev, stream):
+    torch = _T()
+    if not (rows > 0 and V > 0 and K > 0):       # left to the library's validation
+        return _ptr(Z), _ptr(T), _ptr(idx), _ptr(w)
+    top = (rows - 1) * ldt + K
+    return (_addr(Z, "Z", st, (rows - 1) * ldz + V, dev, stream), _addr(T, "T", tt, top, dev, stream),
+            _addr(idx, "idx", torch.int64, top, dev, stream), _addr_or_none(w, "w", torch.float32, rows, dev, stream))
 
 
 def lrc_distill(Z, T, idx, w, loss, lse, dZ, rows: int, V: int, K: int, ldz: int, ldt: int, lddz: int, tau: float, fmt,
                 tfmt, stream=None):
     """Distillation loss of each row of Z against the teacher's top logits T at
     idx, and its gradient dZ; w, loss, lse and dZ may be None."""
-    f, ft, dev = _fmt(fmt), _fmt(tfmt), _call_device(stream)
-    f32 = _T().float32
-    _check_distill(Z, T, idx, w, dZ, rows, V, K, ldz, ldt, lddz, f, ft, dev, stream)
-    _check_optional(loss, "loss", f32, rows, dev, stream)
-    _check_optional(lse, "lse", f32, rows, dev, stream)
-    _check(load().lrc_distill(_ptr(Z), _ptr(T), _ptr(idx), _ptr(w), _ptr(loss), _ptr(lse), _ptr(dZ), rows, V, K, ldz,
-                              ldt, lddz, float(tau), f, ft, _stream(stream)))
+    (f, st, _), (ft, tt, _), dev, f32 = _types(fmt), _types(tfmt), _call_device(stream), _T().float32
+    z, t, i, wp = _distill_addrs(Z, T, idx, w, rows, V, K, ldz, ldt, st, tt, dev, stream)
+    d = _addr_or_none(dZ, "dZ", st, _extent(rows, V, lddz), dev, stream)
+    lo = _addr_or_none(loss, "loss", f32, rows, dev, stream)
+    ls = _addr_or_none(lse, "lse", f32, rows, dev, stream)
+    _check(load().lrc_distill(z, t, i, wp, lo, ls, d, rows, V, K, ldz, ldt, lddz, tau, f, ft, _handle(stream, dev)))
 
 
 def lrc_distill_grad(Z, T, idx, w, lse, g, dZ, rows: int, V: int, K: int, ldz: int, ldt: int, lddz: int, tau: float, fmt,
                      tfmt, stream=None):
     """Gradient of lrc_distill's losses apart, from its lse; w and g may be None."""
-    f, ft, dev = _fmt(fmt), _fmt(tfmt), _call_device(stream)
-    f32 = _T().float32
-    _check_distill(Z, T, idx, w, dZ, rows, V, K, ldz, ldt, lddz, f, ft, dev, stream)
+    (f, st, _), (ft, tt, _), dev, f32 = _types(fmt), _types(tfmt), _call_device(stream), _T().float32
+    z, t, i, wp = _distill_addrs(Z, T, idx, w, rows, V, K, ldz, ldt, st, tt, dev, stream)
     if rows > 0:
-        _check_arg(lse, "lse", f32, rows, dev, stream)
-        _check_optional(g, "g", f32, rows, dev, stream)
-        _check_arg(dZ, "dZ", storage_dtype(f), 0, dev, stream)
-    _check(load().lrc_distill_grad(_ptr(Z), _ptr(T), _ptr(idx), _ptr(w), _ptr(lse), _ptr(g), _ptr(dZ), rows, V, K, ldz,
-                                   ldt, lddz, float(tau), f, ft, _stream(stream)))
+        ls = _addr(lse, "lse", f32, rows, dev, stream)
+        gp = _addr_or_none(g, "g", f32, rows, dev, stream)
+        d = _addr(dZ, "dZ", st, _extent(rows, V, lddz), dev, stream)
+    else:
+        ls, gp, d = _ptr(lse), _ptr(g), _ptr(dZ)
+    _check(load().lrc_distill_grad(z, t, i, wp, ls, gp, d, rows, V, K, ldz, ldt, lddz, tau, f, ft,
+                                   _handle(stream, dev)))
 
 
 # --------------------------------------------------------------------------

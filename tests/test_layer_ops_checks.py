@@ -107,13 +107,20 @@ def test_distill_refusals(L):              # noqa: F811
     assert grad(lse=None) == -1 and grad(dZ=None) == -1 and grad(g=P + 2) == -2
 
 
+class Stand(AsCuda):
+    """With an address: a call whose other arguments are wrong takes it, and goes no further."""
+
+    def data_ptr(self):
+        return P
+
+
 @pytest.fixture
 def current_device_0(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
 
 
 def test_binding_refusals(current_device_0):
-    h = lambda shape, dt=torch.float32: AsCuda(torch.zeros(shape, dtype=dt))      # noqa: E731
+    h = lambda shape, dt=torch.float32: Stand(torch.zeros(shape, dtype=dt))      # noqa: E731
     Q, s, z = h((4, 64), torch.uint8), h((2, 16)), h((2, 16), torch.uint8)
     with pytest.raises(ValueError, match="CUDA tensor"):
         lrc.lrc_q4_apply(torch.zeros((4, 64), dtype=torch.uint8), s, z, h((1, 64)), None, h((1, 4)), 4, 60, 1, 32, "f32")
