@@ -432,7 +432,7 @@ lrc_status lrc_device_status(lrc_stream_t stream) {
     const uint32_t t3 = take_tt3_tc_error();
     const uint32_t tn = take_ttn_tc_error();
     const uint32_t sk = take_skinny_error() | take_split_error() | take_split32_error();
-    const uint32_t q4 = take_q4_error(), ln = take_norm_error(), ds = take_distill_error();
+    const uint32_t q4 = take_q4_error() | take_q4_wide_error(), ln = take_norm_error(), ds = take_distill_error();
     const uint32_t t = t1 | t3 | tn;
     if (q4 == 0xffffffffu || ln == 0xffffffffu || ds == 0xffffffffu || a == 0xffffffffu || t1 == 0xffffffffu || t3 == 0xffffffffu || tn == 0xffffffffu || sk == 0xffffffffu) {
         set_error("could not read the device error words");

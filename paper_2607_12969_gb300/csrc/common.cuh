@@ -218,6 +218,7 @@ uint32_t take_skinny_error();
 uint32_t take_split_error();
 uint32_t take_split32_error();
 uint32_t take_q4_error();
+uint32_t take_q4_wide_error();
 uint32_t take_norm_error();
 uint32_t take_distill_error();
 lrc_status launch_wait_timeout_probe(int64_t limit_ns, cudaStream_t s);

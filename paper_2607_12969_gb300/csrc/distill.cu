@@ -19,6 +19,7 @@
 // the teacher's entries the gradient is written once more at the end of the row.
 #include <math.h>
 
+#include "cluster.cuh"
 #include "common.cuh"
 #include "elem.cuh"
 #include "tc.cuh"
@@ -113,48 +114,6 @@ struct Running {
     }
 };
 
-__device__ __forceinline__ uint32_t cluster_size() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_store(float* p, uint32_t rank, float v) {
-    uint32_t at;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(p)), "r"(rank));
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
-}
-__device__ __forceinline__ void cluster_arrive(uint64_t* bar, uint32_t rank) {
-    uint32_t at;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(bar)), "r"(rank));
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at) : "memory");
-}
-// (Within a limit of time, like every wait of the kernel.)
-__device__ __forceinline__ void cluster_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
-    const uint64_t t0 = tc::globaltimer();
-    while (true) {
-        uint32_t ok;
-        asm volatile(
-            "{\n .reg .pred p;\n"
-            " mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-            " selp.u32 %0, 1, 0, p;\n}\n"
-            : "=r"(ok) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
-        if (ok || *abort) return;
-        if (tc::globaltimer() - t0 > tc::kWaitLimitNs) {
-            atomicOr(&g_err_distill, 2u);
-            *abort = 1;
-            return;
-        }
-    }
-}
-
 // What the teacher's warp leaves for a row.
 struct Teacher {
     float c;                 // tau w g, 0 where the row has no gradient
@@ -183,7 +142,7 @@ __global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_k
     int* tables = reinterpret_cast<int*>(zk + kAhead * a.K);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t ranks = cluster_size(), rank = cluster_rank();
+    const uint32_t ranks = cl::size(), rank = cl::rank();
     const int clusters = gridDim.x / ranks, first = blockIdx.x / ranks;
     const int64_t c0 = rank * a.slice;
     const int len = (int)min(a.slice, a.V - c0);              // elements of this block's slice
@@ -206,7 +165,7 @@ __global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_k
         for (int p = 0; p < 2; ++p) tc::mbar_init(&got[p], ranks);
         tc::fence_barrier_init();
     }
-    if (ranks > 1) cluster_sync();                            // every block's barriers are there
+    if (ranks > 1) cl::sync();                            // every block's barriers are there
     else __syncthreads();
     tc::pdl_wait();
     tc::pdl_trigger();
@@ -333,11 +292,11 @@ __global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_k
         // teacher's places' logits, which may lie where it is written.)
         auto exchange = [&](int p, int r, float m, float s) {
             if (threadIdx.x < ranks) {
-                cluster_store(&all_m[p][rank], threadIdx.x, m);
-                cluster_store(&all_s[p][rank], threadIdx.x, s);
-                cluster_arrive(&got[p], threadIdx.x);
+                cl::store(&all_m[p][rank], threadIdx.x, m);
+                cl::store(&all_s[p][rank], threadIdx.x, s);
+                cl::arrive(&got[p], threadIdx.x);
             }
-            cluster_wait(&got[p], r >> 1 & 1, abort);
+            cl::wait(&got[p], r >> 1 & 1, abort, &g_err_distill, 2u);
         };
         int ahead = -1;                      // the row's teacher entries
         uint32_t tphase = 1;
@@ -499,7 +458,7 @@ __global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_k
             if (lane == 0) tc::mbar_arrive(&tempty[ahead]);
         }
     }
-    if (ranks > 1) cluster_sync();           // no block ends before the others have given it theirs
+    if (ranks > 1) cl::sync();           // no block ends before the others have given it theirs
 }
 
 constexpr int kSmem = 216 * 1024;            // of a multiprocessor, for rings and teacher entries

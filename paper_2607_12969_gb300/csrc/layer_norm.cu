@@ -9,6 +9,7 @@
 // sums and its result (in registers, in the gradient also in shared memory).
 #include <type_traits>
 
+#include "cluster.cuh"
 #include "common.cuh"
 #include "elem.cuh"
 #include "tc.cuh"
@@ -19,8 +20,6 @@ namespace {
 using bf16 = __nv_bfloat16;
 
 __device__ unsigned int g_err_norm;
-
-constexpr int kGroup = 8;          // elements of a thread's vector
 
 // ---- elements of a row -------------------------------------------------------
 
@@ -326,50 +325,6 @@ struct GradArgs {
     int pk;
 };
 
-__device__ __forceinline__ uint32_t cluster_size() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// Writes v to the place of *p in the shared memory of block `rank` of the cluster.
-__device__ __forceinline__ void cluster_store(float* p, uint32_t rank, float v) {
-    uint32_t at;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(p)), "r"(rank));
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
-}
-// Arrives at the barrier in the place of *bar of block `rank`: what the thread has
-// written before is there for those who wait with cluster_wait.
-__device__ __forceinline__ void cluster_arrive(uint64_t* bar, uint32_t rank) {
-    uint32_t at;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(bar)), "r"(rank));
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at) : "memory");
-}
-__device__ __forceinline__ void cluster_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
-    const uint64_t t0 = tc::globaltimer();
-    while (true) {
-        uint32_t ok;
-        asm volatile(
-            "{\n .reg .pred p;\n"
-            " mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-            " selp.u32 %0, 1, 0, p;\n}\n"
-            : "=r"(ok) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
-        if (ok || *abort) return;
-        if (tc::globaltimer() - t0 > tc::kWaitLimitNs) {
-            atomicOr(&g_err_norm, 2u);
-            *abort = 1;
-            return;
-        }
-    }
-}
-
 // Where the rows of a tensor start within 16 bytes: their copies keep it, so that
 // whole 16 bytes of a row go by one bulk copy and its first and last elements by
 // plain loads.  Nothing beside the row is read.
@@ -405,7 +360,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_kernel(const __grid
     __shared__ uint64_t full[kMostRing], got[2];
     __shared__ int abort_flag;
     const int T = blockDim.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t ranks = cluster_size(), rank = cluster_rank();
+    const uint32_t ranks = cl::size(), rank = cl::rank();
     const int clusters = gridDim.x / ranks, first = blockIdx.x / ranks;
     const int64_t c0 = rank * a.slice;
     const int cols = (int)min(a.slice, a.cols - c0);                       // this block's columns
@@ -420,7 +375,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_kernel(const __grid
         for (int p = 0; p < 2; ++p) tc::mbar_init(&got[p], ranks * 2);
         tc::fence_barrier_init();
     }
-    if (ranks > 1) cluster_sync();           // every block's barriers are there
+    if (ranks > 1) cl::sync();           // every block's barriers are there
     else __syncthreads();
     tc::pdl_wait();
     tc::pdl_trigger();
@@ -565,10 +520,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_kernel(const __grid
             // they had read those of row k.)
             if (warp == 0 && l == 0)
                 for (uint32_t w = 0; w < ranks; ++w) {
-                    cluster_store(&totals[p][rank][lane >> 4], w, both);
-                    cluster_arrive(&got[p], w);
+                    cl::store(&totals[p][rank][lane >> 4], w, both);
+                    cl::arrive(&got[p], w);
                 }
-            cluster_wait(&got[p], turn, abort);
+            cl::wait(&got[p], turn, abort, &g_err_norm, 2u);
             both = 0.f;
             for (uint32_t w = 0; w < ranks; ++w) both += totals[p][w][lane >> 4];
             turn ^= p;
@@ -620,7 +575,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_kernel(const __grid
             }
         }
     }
-    if (ranks > 1) cluster_sync();           // no block ends before the others have given it theirs
+    if (ranks > 1) cl::sync();           // no block ends before the others have given it theirs
 }
 
 // Rows too long for that: dx a row a block, the columns' sums apart.

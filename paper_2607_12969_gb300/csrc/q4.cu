@@ -8,14 +8,12 @@
 
 #include <atomic>
 
-#include "common.cuh"
-#include "elem.cuh"
-#include "tc.cuh"
+#include "q4.cuh"
 
 namespace lrc {
 namespace {
 
-using bf16 = __nv_bfloat16;
+using namespace q4;
 
 constexpr float kSeventh = 0.14285714285714285f;      // binary32 next to 1/7
 constexpr float kFifteenth = 0.06666666666666667f;    // and to 1/15
@@ -223,98 +221,7 @@ q4_widen_kernel(const uint32_t* __restrict__ Q, const S* __restrict__ scales, co
 // What bounds it: the unpacking, 11 (bfloat16) or 9 (binary16) instructions for
 // eight codes, 7 or 5 of them on the pipe of half rate; and HBM.
 
-// (a & mask) | bits as one instruction.
-template <uint32_t MASK, uint32_t BITS>
-__device__ __forceinline__ uint32_t pick(uint32_t a) {
-    uint32_t d;
-    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(a), "n"(MASK), "n"(BITS));
-    return d;
-}
-
-struct Half2 {
-    using type = __half;
-    // The eight q - z of a word, in order.  1024 + q for the codes in the low four
-    // bits of a byte; 1024 + 16 q for the others, brought to q - z by one exact
-    // multiply-add instead of a shift (shifts and masks share a pipe of half the
-    // multiply-adds' rate, which is what the kernel would wait for).
-    static __device__ __forceinline__ void unpack(uint32_t w, uint32_t z, uint32_t (&r)[4]) {
-        const uint32_t one = 0x64006400u + z * 0x10001u;       // 1024 + z
-        const uint32_t sixteenth = 0x2c002c00u;                // 1 / 16
-        const uint32_t less = 0xd400d400u + z * 0x00100010u;   // -(64 + z)
-        const uint32_t w8 = w >> 8;
-        const uint32_t lo0 = pick<0x000f000fu, 0x64006400u>(w), hi0 = pick<0x00f000f0u, 0x64006400u>(w);
-        const uint32_t lo1 = pick<0x000f000fu, 0x64006400u>(w8), hi1 = pick<0x00f000f0u, 0x64006400u>(w8);
-        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r[0]) : "r"(lo0), "r"(one));
-        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r[1]) : "r"(hi0), "r"(sixteenth), "r"(less));
-        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r[2]) : "r"(lo1), "r"(one));
-        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r[3]) : "r"(hi1), "r"(sixteenth), "r"(less));
-    }
-    static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                               uint32_t b0, uint32_t b1) {
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-    }
-    // The same with nothing to add to.
-    static __device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                                     uint32_t b0, uint32_t b1) {
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
-    }
-};
-struct Bf2 {
-    using type = bf16;
-    // 128 + q has no room for a code above the low four bits: a shift for each.
-    // (The upper halves of products with 2^28, 2^24, 2^20 in the place of shifts,
-    // on the multipliers' pipe, are slower: 47 us against 43 for 16384 x 16384.)
-    static __device__ __forceinline__ void unpack(uint32_t w, uint32_t z, uint32_t (&r)[4]) {
-        const uint32_t less = 0x43004300u + z * 0x10001u;      // 128 + z
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const uint32_t a = pick<0x000f000fu, 0x43004300u>(w >> (4 * u));
-            asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r[u]) : "r"(a), "r"(less));
-        }
-    }
-    static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                               uint32_t b0, uint32_t b1) {
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-    }
-    // The same with nothing to add to.
-    static __device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                                     uint32_t b0, uint32_t b1) {
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
-    }
-};
-
-struct ApplyArgs {
-    const uint4* Q;          // m rows of 4 blocks uint4
-    const void* scales;
-    const uint8_t* zeros;
-    const void* x;           // cols rows of 16-bit elements, pitch ldx
-    const void* A;
-    void* y;
-    int64_t m, blocks, groups, ldm, ldx, xcols;
-    int cols, xrows;         // rows of x (vectors, or three parts of each), and of its boxes
-    int R, split, depth;     // groups of 16 rows of a tile; blocks of a cluster; stages of the ring
-    bool wide;               // A and y are binary32
-};
-
 __device__ unsigned int g_err_q4;
-
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// The float at the same place of the shared memory of block `rank` of the cluster.
-__device__ __forceinline__ float cluster_load(const float* p, uint32_t rank) {
-    uint32_t at;
-    float v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-    return v;
-}
 
 // Shared memory of a stage of 512 columns for 16 R rows: two boxes of 128 bytes of
 // codes a row, eight boxes of 64 columns of x (kCols rows of 128 bytes), all with
@@ -336,8 +243,6 @@ struct StageOf {
 // Groups of 16 rows of a tile at most: 15 warps of a block have 128 registers a
 // thread, 17 would have 96.
 constexpr int kMostRows = 7;
-// Columns of B that a tile uses: whole vectors.
-constexpr int used_cols(int NT, int PARTS) { return 8 * NT / PARTS * PARTS; }
 constexpr int kMostDepth = 8;      // stages of a ring
 
 // OP: the instructions' element type; S: the scales' type; PARTS: columns of B
@@ -356,7 +261,7 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = 2 * a.R, threads = 64 * a.R + 32;
     const int rows = 16 * a.R, rank = blockIdx.x % a.split;
     const int64_t row0 = (int64_t)(blockIdx.x / a.split) * rows;
-    const int col0 = blockIdx.y * used_cols(NT, PARTS);
+    const int col0 = blockIdx.y * used_cols(8 * NT, PARTS);
     const int stages = (int)((a.blocks + 3) / 4);
     const int mine = (stages - rank + a.split - 1) / a.split;         // stages of this block
     uint8_t* ring = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
@@ -488,9 +393,9 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             for (int u = 0; u < 4; ++u)      // column 2 t + u of eight, t or t + 4 of the vectors
                 sums[(half * kCols + 8 * c + t + 4 * (u & 1)) * pitch + row + 8 * (u >> 1)] = acc[c][u];
     }
-    if (a.split > 1) cluster_sync();
+    if (a.split > 1) cl::sync();
     else __syncthreads();
-    const int used = min(a.cols - col0, used_cols(NT, PARTS)) / PARTS;      // vectors of this tile
+    const int used = min(a.cols - col0, used_cols(8 * NT, PARTS)) / PARTS;      // vectors of this tile
     for (int e = rank * threads + threadIdx.x; e < used * rows; e += a.split * threads) {
         const int v = e / rows, r = e % rows;
         if (row0 + r >= a.m) continue;
@@ -501,7 +406,7 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             for (int q = 0; q < 2; ++q) {
                 const float* at = &sums[(q * kCols + v * PARTS + p) * pitch + r];
                 if (a.split > 1)
-                    for (int w = 0; w < a.split; ++w) sum += cluster_load(at, w);
+                    for (int w = 0; w < a.split; ++w) sum += cl::load(at, w);
                 else
                     sum += *at;
             }
@@ -516,7 +421,7 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             static_cast<T*>(a.y)[o] = el::from_f32<T>(sum);
         }
     }
-    if (a.split > 1) cluster_sync();                              // the sums stay until they are read
+    if (a.split > 1) cl::sync();                              // the sums stay until they are read
 }
 
 lrc_status grid_of(int64_t threads, int per, const char* what, unsigned* out) {
@@ -594,12 +499,6 @@ q4_parts_kernel(const float* __restrict__ x, int64_t n, int64_t ldn, int64_t ldp
     p[2 * ldp] = (uint16_t)(__float_as_uint(last) >> 16);
 }
 
-constexpr CUtensorMapDataType map_type(float) { return CU_TENSOR_MAP_DATA_TYPE_FLOAT32; }
-constexpr CUtensorMapDataType map_type(__half) { return CU_TENSOR_MAP_DATA_TYPE_FLOAT16; }
-constexpr CUtensorMapDataType map_type(bf16) { return CU_TENSOR_MAP_DATA_TYPE_BFLOAT16; }
-
-constexpr int kSmemOfSm = 227 * 1024;
-
 // Groups of rows of a tile and blocks of a cluster: what takes the shortest by a
 // model of a multiprocessor's time, in units of what it takes for 16 rows and a
 // stage (0.11 us).  A block needs five such a stage at least however few its rows
@@ -626,7 +525,7 @@ inline void choose_tile(ApplyArgs* a, int chunks) {
 template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NT>
 lrc_status apply_launch(ApplyArgs a, cudaStream_t s) {
     using St = StageOf<S, GROUP, ZEROS, NT>;
-    constexpr int kUsed = used_cols(NT, PARTS);
+    constexpr int kUsed = used_cols(8 * NT, PARTS);
     a.xrows = a.cols < kUsed ? a.cols : kUsed;
     const int chunks = (a.cols + kUsed - 1) / kUsed;
     choose_tile(&a, chunks);
@@ -696,12 +595,15 @@ lrc_status apply_groups(const ApplyArgs& a, int group, cudaStream_t s) {
 // codes as the widest would.
 template <typename OP, typename S, int PARTS>
 lrc_status apply_tiles(const ApplyArgs& a, int group, cudaStream_t s) {
-    const int passes = (a.cols + used_cols(4, PARTS) - 1) / used_cols(4, PARTS);
-    if (used_cols(1, PARTS) * passes >= a.cols) return apply_groups<OP, S, PARTS, 1>(a, group, s);
-    if (used_cols(2, PARTS) * passes >= a.cols) return apply_groups<OP, S, PARTS, 2>(a, group, s);
-    if (used_cols(3, PARTS) * passes >= a.cols) return apply_groups<OP, S, PARTS, 3>(a, group, s);
+    const int passes = (a.cols + used_cols(32, PARTS) - 1) / used_cols(32, PARTS);
+    if (used_cols(8, PARTS) * passes >= a.cols) return apply_groups<OP, S, PARTS, 1>(a, group, s);
+    if (used_cols(16, PARTS) * passes >= a.cols) return apply_groups<OP, S, PARTS, 2>(a, group, s);
+    if (used_cols(24, PARTS) * passes >= a.cols) return apply_groups<OP, S, PARTS, 3>(a, group, s);
     return apply_groups<OP, S, PARTS, 4>(a, group, s);
 }
+
+#define Q4FEW 32
+constexpr int kFew = Q4FEW;
 
 template <typename OP, typename S, typename Y, int PARTS>
 lrc_status apply_as(const void* Q, const void* scales, const uint8_t* zeros, const void* x, const void* A, void* y,
@@ -716,10 +618,12 @@ lrc_status apply_as(const void* Q, const void* scales, const uint8_t* zeros, con
     a.groups = (n + group - 1) / group;
     a.wide = sizeof(Y) == 4;
     const int64_t ldn = lrc_packed_ld(n);
-    // at most this many vectors a launch
-    constexpr int64_t kMost = 16384;
-    for (int64_t b0 = 0; b0 < b; b0 += kMost) {
-        const int64_t nb = b - b0 < kMost ? b - b0 : kMost;
+    // vectors a launch: 16384, of binary32 ones as many as have parts of 256 MB
+    int64_t most = 16384;
+    if (PARTS > 1 && most > (int64_t)(256 << 20) / (a.blocks * 768)) most = (int64_t)(256 << 20) / (a.blocks * 768);
+    if (most < 1) most = 1;
+    for (int64_t b0 = 0; b0 < b; b0 += most) {
+        const int64_t nb = b - b0 < most ? b - b0 : most;
         a.A = A ? (const Y*)A + b0 * m : nullptr;
         a.y = (Y*)y + b0 * m;
         a.cols = (int)nb * PARTS;
@@ -740,7 +644,7 @@ lrc_status apply_as(const void* Q, const void* scales, const uint8_t* zeros, con
             if (e != cudaSuccess) return cuda_fail(e, "q4_parts_kernel");
             if ((st = after_launch("q4_parts_kernel")) != LRC_OK) return st;
         }
-        const lrc_status st = apply_tiles<OP, S, PARTS>(a, group, s);
+        const lrc_status st = a.cols > kFew ? q4::launch_wide<OP, S, PARTS>(a, group, s) : apply_tiles<OP, S, PARTS>(a, group, s);
         if (st != LRC_OK) return st;
     }
     return LRC_OK;
