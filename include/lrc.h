@@ -584,7 +584,10 @@ LRC_API lrc_status lrc_q4_widen(const void* Q, const void* scales, const uint8_t
  * scaled and added in binary32; A is added and the result rounded to Y's type
  * once.  (A group's sum comes before its scale: entries of X above 2^115 could
  * overflow there.)  Deterministic.  Made for the few vectors of a serving step:
- * the weights are read once for up to 64 of them.  Asynchronous on `stream`.
+ * the weights are read once for up to 64 of them, 21 in binary32.  A binary32 X
+ * is split into three bfloat16 parts in the stream's workspace (see lrc_apply),
+ * 6 bytes an element, at most 256 MB of them, or one vector's, at a time (a
+ * larger X takes several launches).  Asynchronous on `stream`.
  */
 LRC_API lrc_status lrc_q4_apply(const void* Q, const void* scales, const uint8_t* zeros, const void* X, const void* A,
                                 void* Y, int64_t m, int64_t n, int64_t b, int64_t group, lrc_fmt fmt,

@@ -10,8 +10,11 @@ sizes or devices).  There is no CPU fallback: if the library is missing or
 fails to load, every call raises.
 
 Names follow the C ABI: lrc_round_factors, lrc_widen_factors, lrc_apply,
-tt_reconstruct, lrc_fro_diff, plus the host helpers lrc_certified,
-lrc_tail_error, lrc_matrix_storage_ratio and lrc_tt_storage_bytes.
+tt_reconstruct, lrc_fro_diff; for a compressed layer's 4-bit remainder and the
+steps around it lrc_q4_round, lrc_q4_widen, lrc_q4_apply, lrc_layer_norm,
+lrc_layer_norm_grad, lrc_distill and lrc_distill_grad; plus the host helpers
+lrc_certified, lrc_tail_error, lrc_matrix_storage_ratio and
+lrc_tt_storage_bytes.
 """
 from __future__ import annotations
 

@@ -27,9 +27,10 @@ __device__ __forceinline__ uint32_t place(const void* p, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(p)), "r"(rank));
     return at;
 }
-__device__ __forceinline__ float load(const float* p, uint32_t rank) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(place(p, rank)) : "memory");
+__device__ __forceinline__ float4 load4(const float* p, uint32_t rank) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(place(p, rank)) : "memory");
     return v;
 }
 __device__ __forceinline__ void store(float* p, uint32_t rank, float v) {

@@ -385,7 +385,7 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     __syncthreads();                                              // the ring is free
     // sums[half][column][row]
     float* sums = reinterpret_cast<float*>(ring);
-    const int pitch = rows + 1;
+    const int pitch = rows + 4;
     if (warp < warps) {
 #pragma unroll
         for (int c = 0; c < NT; ++c)
@@ -396,31 +396,7 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     if (a.split > 1) cl::sync();
     else __syncthreads();
     const int used = min(a.cols - col0, used_cols(8 * NT, PARTS)) / PARTS;      // vectors of this tile
-    for (int e = rank * threads + threadIdx.x; e < used * rows; e += a.split * threads) {
-        const int v = e / rows, r = e % rows;
-        if (row0 + r >= a.m) continue;
-        float sum = 0.f;
-#pragma unroll
-        for (int p = PARTS - 1; p >= 0; --p) {                    // the smallest part first
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const float* at = &sums[(q * kCols + v * PARTS + p) * pitch + r];
-                if (a.split > 1)
-                    for (int w = 0; w < a.split; ++w) sum += cl::load(at, w);
-                else
-                    sum += *at;
-            }
-        }
-        const int64_t o = (int64_t)(col0 / PARTS + v) * a.m + row0 + r;
-        if (PARTS > 1 || a.wide) {
-            if (a.A) sum += static_cast<const float*>(a.A)[o];
-            static_cast<float*>(a.y)[o] = sum;
-        } else {
-            using T = typename OP::type;
-            if (a.A) sum += el::to_f32(static_cast<const T*>(a.A)[o]);
-            static_cast<T*>(a.y)[o] = el::from_f32<T>(sum);
-        }
-    }
+    finish_tile<OP, PARTS, 2>(a, sums, kCols * pitch, pitch, rows, row0, col0, used, rank, threads);
     if (a.split > 1) cl::sync();                              // the sums stay until they are read
 }
 
@@ -602,8 +578,12 @@ lrc_status apply_tiles(const ApplyArgs& a, int group, cudaStream_t s) {
     return apply_groups<OP, S, PARTS, 4>(a, group, s);
 }
 
-#define Q4FEW 32
-constexpr int kFew = Q4FEW;
+// Columns up to which the product is mma.sync's.  Either way one pass over the codes;
+// this one's warps hand nothing on, so it starts sooner: 1000 x 4000 and 30 bfloat16
+// vectors 7.4 us here, 11.2 on tcgen05; 12287 x 16381 and 10 binary32 vectors (30
+// columns) 50 and 76; 16384 x 8192 and 32 binary16 vectors 29.9 and 27.2.  Above, this
+// one would pass over the codes again: 48 vectors 52 us here, 32 there.
+constexpr int kFew = 32;
 
 template <typename OP, typename S, typename Y, int PARTS>
 lrc_status apply_as(const void* Q, const void* scales, const uint8_t* zeros, const void* x, const void* A, void* y,

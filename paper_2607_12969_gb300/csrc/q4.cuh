@@ -102,6 +102,49 @@ constexpr CUtensorMapDataType map_type(bf16) { return CU_TENSOR_MAP_DATA_TYPE_BF
 
 constexpr int kSmemOfSm = 227 * 1024;
 
+// The end of a tile: sums of SETS sets (set s, column c, row r of the tile at sums[s *
+// set + c * pitch + r], pitch a multiple of four) and of the blocks of the cluster,
+// added in a fixed order, four rows a thread; then A and the rounding.  All loads of
+// other blocks are on their way before the first is added: one after the other, their
+// latency was up to half of a small product's time.
+template <typename OP, int PARTS, int SETS>
+__device__ __forceinline__ void finish_tile(const ApplyArgs& a, const float* sums, int set, int pitch, int rows,
+                                            int64_t row0, int col0, int vectors, int rank, int threads) {
+    const int quads = rows / 4;
+    for (int e = rank * threads + (int)threadIdx.x; e < vectors * quads; e += a.split * threads) {
+        const int v = e / quads, r = e % quads * 4;
+        if (row0 + r >= a.m) continue;
+        float sum[4] = {};
+#pragma unroll
+        for (int p = PARTS - 1; p >= 0; --p)                      // the smallest part first
+#pragma unroll
+            for (int s = 0; s < SETS; ++s) {
+                const float* at = sums + s * set + (v * PARTS + p) * pitch + r;
+                float4 w[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    if (q < a.split) w[q] = a.split > 1 ? cl::load4(at, q) : *reinterpret_cast<const float4*>(at);
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    if (q < a.split) sum[0] += w[q].x, sum[1] += w[q].y, sum[2] += w[q].z, sum[3] += w[q].w;
+            }
+        const int64_t o = (int64_t)(col0 / PARTS + v) * a.m + row0 + r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (row0 + r + i >= a.m) break;
+            float y = sum[i];
+            if (PARTS > 1 || a.wide) {
+                if (a.A) y += static_cast<const float*>(a.A)[o + i];
+                static_cast<float*>(a.y)[o + i] = y;
+            } else {
+                using T = typename OP::type;
+                if (a.A) y += el::to_f32(static_cast<const T*>(a.A)[o + i]);
+                static_cast<T*>(a.y)[o + i] = el::from_f32<T>(y);
+            }
+        }
+    }
+}
+
 // The product of more vectors (q4_wide.cu); parts: columns that make one vector.
 template <typename OP, typename S, int PARTS>
 lrc_status launch_wide(ApplyArgs a, int group, cudaStream_t s);

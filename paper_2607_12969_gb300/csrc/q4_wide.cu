@@ -2,20 +2,23 @@
 // fifth-generation tensor cores (tcgen05, accumulators and the matrix in tensor
 // memory).
 //
-// A tile is 128 rows of the matrix and NC columns of vectors.  One warp brings
-// blocks of 128 columns by TMA; three groups of four warps take every third block
-// each: a thread unpacks its row's 128 codes to the integers q - z, exact in 16
-// bits, and writes them to tensor memory as the A operand, one thread issues the
-// products with the block's x (B, in shared memory as TMA wrote it), and every
-// thread adds its row's sums of each group times the scale in binary32.  So the
-// codes are unpacked once for all columns, and neither they nor the sums pass
-// through shared memory.  The three groups' sums, and those of the blocks of a
-// cluster, which share the columns of the matrix, are added at the end in a fixed
-// order.
+// A tile is 256 rows of the matrix and NC columns of vectors, 128 columns of the
+// matrix (a block) at a time, brought by TMA.  Two pairs of teams of four warps take
+// every second block each, a team of a pair half of the rows: a thread unpacks its
+// row's 128 codes to the integers q - z, exact in 16 bits, and writes them to tensor
+// memory as the A operand, one thread issues the products with the block's x (B, in
+// shared memory as TMA wrote it), and every thread adds its row's sums of each group
+// times the scale in binary32.  So the codes are unpacked once for all columns, and
+// neither they nor the sums pass through shared memory.  The pairs' sums, and those
+// of the blocks of a cluster, which share the columns of the matrix, are added at
+// the end in a fixed order.
 //
-// What bounds it: the unpacking (as in q4.cu), the adding of NC sums a row and
-// group, and the chain of a block (unpack, write, multiply, read), of which the
-// three groups have one each in flight.
+// What bounds it: for 16384 x 8192 and 64 binary16 vectors (33 us) the chain of a
+// block (unpack, write, multiply, read, add), of which a multiprocessor has four in
+// flight -- all of tensor memory is in use -- and the polling of those who wait;
+// leaving out any one step of it gains 1 to 7 us.  With 128 rows a tile (34 us) the
+// vectors pass the multiprocessors' L2 ports twice as often: 128 vectors 65 us
+// against 56.  Four kinds of warps that hand blocks on took 57 us.
 #include "q4.cuh"
 
 #include <math.h>
@@ -29,9 +32,10 @@ using namespace q4;
 
 __device__ unsigned int g_err_q4_wide;
 
-constexpr int kTeams = 3, kTeamThreads = 128, kThreads = kTeams * kTeamThreads + 32;
+constexpr int kPairs = 2, kTeams = 2 * kPairs, kTeamThreads = 128, kThreads = kTeams * kTeamThreads;
+constexpr int kRows = 256;
 constexpr uint32_t kTmem = 512, kACols = 64;      // columns of tensor memory; of a team's A (128 x 128 of 16 bits)
-constexpr int kMostStages = 16;
+constexpr int kMostStages = 4;                    // of a pair
 
 // D[tmem] (+)= A[tmem] B[smem]^T, 128 x N x 16; one thread issues.
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
@@ -48,19 +52,19 @@ __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) 
         "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 
-// Shared memory of a stage, one block of 128 columns: 128 rows of 64 bytes of codes
+// Shared memory of a stage, one block of 128 columns: kRows rows of 64 bytes of codes
 // (64-byte swizzle), two boxes of 64 columns of x (NC rows of 128 bytes, 128-byte
-// swizzle), scales and zero codes of the groups, 128 a group.
+// swizzle), scales and zero codes of the groups, kRows a group.
 template <typename S, int GROUP, bool ZEROS, int NC>
 struct WideStage {
-    static constexpr int kGroups = 128 / GROUP, kX = 8192, kXBox = NC * 128, kScales = kX + 2 * kXBox;
-    static constexpr int kScaleBytes = kGroups * 128 * (int)sizeof(S), kZeros = kScales + kScaleBytes;
-    static constexpr int kZeroBytes = ZEROS ? kGroups * 128 : 0;
+    static constexpr int kGroups = 128 / GROUP, kX = kRows * 64, kXBox = NC * 128, kScales = kX + 2 * kXBox;
+    static constexpr int kScaleBytes = kGroups * kRows * (int)sizeof(S), kZeros = kScales + kScaleBytes;
+    static constexpr int kZeroBytes = ZEROS ? kGroups * kRows : 0;
     static constexpr int kPitch = (kZeros + kZeroBytes + 1023) / 1024 * 1024;
-    static constexpr int kSums = kTeams * NC * 129 * 4;
-    static constexpr int kRoom = (kSmemOfSm - 3072) / kPitch;
-    static constexpr int kDepth = kRoom < kMostStages ? kRoom : kMostStages;
-    static_assert(kSums <= kDepth * kPitch, "the sums lie in the ring");
+    static constexpr int kSums = kPairs * NC * (kRows + 4) * 4;
+    static constexpr int kRoom = (kSmemOfSm - 3072) / kPitch / kPairs;
+    static constexpr int kDepth = kRoom < kMostStages ? kRoom : kMostStages;        // stages of a pair
+    static_assert(kDepth >= 2 && kSums <= kPairs * kDepth * kPitch, "the sums lie in the ring");
 };
 
 template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NC>
@@ -73,26 +77,27 @@ q4_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     // sums of so many groups fit into a team's share of tensor memory at once
     constexpr int kAtOnce = kGroups == 1 ? 1 : NC > 32 ? 1 : 2;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t full[kDepth], empty[kDepth], done[kTeams];
+    __shared__ uint64_t full[kPairs][kDepth], empty[kPairs][kDepth], done[kTeams];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp >> 2;
+    const int warp = threadIdx.x >> 5, team = warp >> 2, pair = team >> 1, half = team & 1;
     const int rank = blockIdx.x % a.split;
-    const int64_t row0 = (int64_t)(blockIdx.x / a.split) * 128;
+    const int64_t row0 = (int64_t)(blockIdx.x / a.split) * kRows;
     const int col0 = blockIdx.y * used_cols(NC, PARTS);
     const int mine = (int)((a.blocks - rank + a.split - 1) / a.split);       // blocks of columns
-    uint8_t* ring = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
+    uint8_t* base = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
     volatile int* abort = &abort_flag;
     if (threadIdx.x == 0) {
         abort_flag = 0;
-        for (int d = 0; d < kDepth; ++d) {
-            tc::mbar_init(&full[d], 1);
-            tc::mbar_init(&empty[d], 1);
-        }
+        for (int p = 0; p < kPairs; ++p)
+            for (int d = 0; d < kDepth; ++d) {
+                tc::mbar_init(&full[p][d], 1);
+                tc::mbar_init(&empty[p][d], 2);
+            }
         for (int t = 0; t < kTeams; ++t) tc::mbar_init(&done[t], 1);
         tc::fence_barrier_init();
     }
-    if (warp == 4 * kTeams) tc::tmem_alloc(&tmem_slot, kTmem);
+    if (warp == 0) tc::tmem_alloc(&tmem_slot, kTmem);
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
@@ -101,56 +106,46 @@ q4_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     tc::pdl_trigger();
 
     float acc[NC] = {};
-    if (team == kTeams) {
-        if (lane == 0) {
-            const uint32_t bytes = 8192 + a.xrows * 256 + St::kScaleBytes + St::kZeroBytes;
-            int k = 0, slot = 0;
-            uint32_t phase = 1;
-            for (; k < mine; ++k) {
-                if (k >= kDepth && !tc::mbar_wait(&empty[slot], phase, abort, &g_err_q4_wide, 1u)) break;
-                uint64_t* bar = &full[slot];
-                uint8_t* to = ring + slot * St::kPitch;
-                const int unit = rank + k * a.split;
-                tc::mbar_arrive_expect_tx(bar, bytes);
-                tc::tma_load_2d(to, &qmap, unit * 64, (int32_t)row0, bar);
-                tc::tma_load_2d(to + St::kX, &xmap, unit * 128, col0, bar);
-                tc::tma_load_2d(to + St::kX + St::kXBox, &xmap, unit * 128 + 64, col0, bar);
-                tc::tma_load_2d(to + St::kScales, &smap, (int32_t)row0, unit * kGroups, bar);
-                if (ZEROS) tc::tma_load_2d(to + St::kZeros, &zmap, (int32_t)row0, unit * kGroups, bar);
-                if (++slot == kDepth) {
-                    slot = 0;
-                    phase ^= 1;
-                }
-            }
-            // no copy is in flight when the block goes on
-            volatile int no_abort = 0;
-            for (int u = k > kDepth ? k - kDepth : 0; u < k; ++u)
-                tc::mbar_wait(&full[u % kDepth], u / kDepth & 1, &no_abort, &g_err_q4_wide, 1u);
-        }
-        __syncwarp();
-    } else {
-        const int r = threadIdx.x & 127;                         // row of the tile, lane of tensor memory
+    uint8_t* ring = base + pair * kDepth * St::kPitch;
+    // the pair's n-th block, block 2 n + pair of the tile's, into its stage
+    auto issue = [&](int n) {
+        uint64_t* bar = &full[pair][n % kDepth];
+        uint8_t* to = ring + n % kDepth * St::kPitch;
+        const int unit = rank + (n * kPairs + pair) * a.split;
+        tc::mbar_arrive_expect_tx(bar, kRows * 64 + a.xrows * 256 + St::kScaleBytes + St::kZeroBytes);
+        tc::tma_load_2d(to, &qmap, unit * 64, (int32_t)row0, bar);
+        tc::tma_load_2d(to + St::kX, &xmap, unit * 128, col0, bar);
+        tc::tma_load_2d(to + St::kX + St::kXBox, &xmap, unit * 128 + 64, col0, bar);
+        tc::tma_load_2d(to + St::kScales, &smap, (int32_t)row0, unit * kGroups, bar);
+        if (ZEROS) tc::tma_load_2d(to + St::kZeros, &zmap, (int32_t)row0, unit * kGroups, bar);
+    };
+    {
+        const int r = threadIdx.x & 127, row = half * 128 + r;   // lane of tensor memory, row of the tile
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;       // the warp's first lane, in bits 16 and up
         const uint32_t ta = tmem + team * kACols, td = tmem + kTeams * kACols + team * (kAtOnce * NC);
         const bool issuer = r == 0;
         const int swz = r >> 1 & 3;
         uint32_t round = 0;
+        const int blocks = (mine - pair + kPairs - 1) / kPairs;
+        int issued = 0;
+        const bool fetcher = half == 0 && r == 96;               // of a warp that waits at the team's barrier
+        if (fetcher)
+            for (; issued < kDepth && issued < blocks; ++issued) issue(issued);
         // After a wait that gave up the blocks go on without waits: the team's threads meet
         // at its barriers for every block.
-        for (int k = team; k < mine; k += kTeams) {
-            const int slot = k % kDepth;
-            uint8_t* from = ring + slot * St::kPitch;
-            tc::mbar_wait(&full[slot], k / kDepth & 1, abort, &g_err_q4_wide, 1u);
-            __syncwarp();
+        for (int k = 0; k < blocks; ++k) {
+            uint8_t* from = ring + k % kDepth * St::kPitch;
+            if ((warp & 3) == 0) tc::mbar_wait(&full[pair][k % kDepth], k / kDepth & 1, abort, &g_err_q4_wide, 1u);
+            tc::named_bar_sync(1 + team, kTeamThreads);
             uint4 w[4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) w[t] = *reinterpret_cast<const uint4*>(from + r * 64 + ((t ^ swz) << 4));
+            for (int t = 0; t < 4; ++t) w[t] = *reinterpret_cast<const uint4*>(from + row * 64 + ((t ^ swz) << 4));
             float s[kGroups];
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) s[g] = el::to_f32(reinterpret_cast<const S*>(from + St::kScales)[g * 128 + r]);
+            for (int g = 0; g < kGroups; ++g) s[g] = el::to_f32(reinterpret_cast<const S*>(from + St::kScales)[g * kRows + row]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {                        // columns 32 j ... 32 j + 31
-                const uint32_t z = ZEROS ? from[St::kZeros + j * 32 / GROUP * 128 + r] : 8u;
+                const uint32_t z = ZEROS ? from[St::kZeros + j * 32 / GROUP * kRows + row] : 8u;
                 uint32_t v[16];
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
@@ -178,9 +173,17 @@ q4_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                             mma_ts(td + (g - g0) * NC, ta + 8 * kk, x[kk >> 2] + 2 * (kk & 3), idesc, i != 0);
                         }
                     tc::mma_commit(&done[team]);
-                    if (g0 + kAtOnce >= kGroups) tc::mma_commit(&empty[slot]);
+                    if (g0 + kAtOnce >= kGroups) tc::mma_commit(&empty[pair][k % kDepth]);
                 }
-                tc::mbar_wait(&done[team], round & 1, abort, &g_err_q4_wide, 2u);
+                if ((warp & 3) == 0) tc::mbar_wait(&done[team], round & 1, abort, &g_err_q4_wide, 2u);
+                // The stage of the block before is free where both teams' products are done
+                // (their codes are in tensor memory).
+                if (fetcher && g0 == 0 && k > 0 && issued < blocks && !*abort) {
+                    tc::mbar_wait(&empty[pair][(k - 1) % kDepth], (k - 1) / kDepth & 1, abort, &g_err_q4_wide, 4u);
+                    if (!*abort) issue(issued++);
+                }
+                __syncwarp();
+                tc::named_bar_sync(1 + team, kTeamThreads);
                 ++round;
                 __syncwarp();
                 tc::tc_fence_after();
@@ -196,50 +199,27 @@ q4_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                     }
             }
         }
-        if (*abort && issuer && round) {
-            // the products in flight end before the block does
+        if (*abort && (issuer || fetcher)) {
+            // the products and copies in flight end before the block does
             volatile int no_abort = 0;
-            tc::mbar_wait(&done[team], (round - 1) & 1, &no_abort, &g_err_q4_wide, 2u, 100000000ull);
+            if (issuer && round) tc::mbar_wait(&done[team], (round - 1) & 1, &no_abort, &g_err_q4_wide, 2u, 100000000ull);
+            for (int u = issued > kDepth ? issued - kDepth : 0; u < issued; ++u)
+                tc::mbar_wait(&full[pair][u % kDepth], u / kDepth & 1, &no_abort, &g_err_q4_wide, 1u, 100000000ull);
         }
     }
     tc::tc_fence_before();
     __syncthreads();                                             // the ring is free
     tc::tc_fence_after();
-    if (warp == 4 * kTeams) tc::tmem_dealloc(tmem, kTmem);
-    // sums[team][column][row]
-    float(*sums)[NC][129] = reinterpret_cast<float(*)[NC][129]>(ring);
-    if (team < kTeams) {
+    __syncwarp();
+    if (warp == 0) tc::tmem_dealloc(tmem, kTmem);
+    // sums[pair][column][row]
+    float(*sums)[NC][kRows + 4] = reinterpret_cast<float(*)[NC][kRows + 4]>(base);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) sums[team][c][threadIdx.x & 127] = acc[c];
-    }
+    for (int c = 0; c < NC; ++c) sums[pair][c][threadIdx.x & (kRows - 1)] = acc[c];
     if (a.split > 1) cl::sync();
     else __syncthreads();
     const int used = min(a.cols - col0, used_cols(NC, PARTS)) / PARTS;       // vectors of this tile
-    for (int e = rank * kThreads + threadIdx.x; e < used * 128; e += a.split * kThreads) {
-        const int v = e >> 7, r = e & 127;
-        if (row0 + r >= a.m) continue;
-        float sum = 0.f;
-#pragma unroll
-        for (int p = PARTS - 1; p >= 0; --p) {                   // the smallest part first
-#pragma unroll
-            for (int t = 0; t < kTeams; ++t) {
-                const float* at = &sums[t][v * PARTS + p][r];
-                if (a.split > 1)
-                    for (int q = 0; q < a.split; ++q) sum += cl::load(at, q);
-                else
-                    sum += *at;
-            }
-        }
-        const int64_t o = (int64_t)(col0 / PARTS + v) * a.m + row0 + r;
-        if (PARTS > 1 || a.wide) {
-            if (a.A) sum += static_cast<const float*>(a.A)[o];
-            static_cast<float*>(a.y)[o] = sum;
-        } else {
-            using T = typename OP::type;
-            if (a.A) sum += el::to_f32(static_cast<const T*>(a.A)[o]);
-            static_cast<T*>(a.y)[o] = el::from_f32<T>(sum);
-        }
-    }
+    finish_tile<OP, PARTS, kPairs>(a, &sums[0][0][0], NC * (kRows + 4), kRows + 4, kRows, row0, col0, used, rank, kThreads);
     if (a.split > 1) cl::sync();                                 // the sums stay until they are read
 }
 
@@ -249,12 +229,14 @@ lrc_status wide_as(ApplyArgs a, cudaStream_t s) {
     constexpr int kUsed = used_cols(NC, PARTS);
     a.xrows = a.cols < kUsed ? a.cols : kUsed;
     const int chunks = (a.cols + kUsed - 1) / kUsed;
-    const int64_t tiles = (a.m + 127) / 128;
+    const int64_t tiles = (a.m + kRows - 1) / kRows;
     // Blocks of a cluster: the number that fills the multiprocessors' waves best, a
-    // wave's start and end taken as 14 blocks of columns.
+    // wave's start and end taken as 14 blocks of columns.  (Clusters of eight blocks
+    // that fill a multiprocessor each do not all find room at once: 4096 x 4096 with 64
+    // vectors took 23 us with them.)
     double best = 1e300;
     const int sms = sm_count();
-    for (int split = 1; split <= 8 && split <= a.blocks; split += split < 4 ? 1 : 2) {
+    for (int split = 1; split <= 4 && split <= a.blocks; ++split) {
         const double cost = ceil((double)tiles * chunks * split / sms) * ((double)((a.blocks + split - 1) / split) + 14.);
         if (cost < best) {
             best = cost;
@@ -262,22 +244,22 @@ lrc_status wide_as(ApplyArgs a, cudaStream_t s) {
         }
     }
     CUtensorMap qm, xm, sm, zm{};
-    lrc_status st = encode_map_2d_sw64(&qm, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.Q, a.blocks * 64, a.m, a.blocks * 64, 64, 128,
+    lrc_status st = encode_map_2d_sw64(&qm, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.Q, a.blocks * 64, a.m, a.blocks * 64, 64, kRows,
                                        "Q");
     if (st != LRC_OK) return st;
     st = encode_map_2d(&xm, map_type(typename OP::type()), a.x, a.xcols, a.cols, a.ldx * 2, 64, (uint32_t)a.xrows, true,
                        "X");
     if (st != LRC_OK) return st;
-    st = encode_map_2d(&sm, map_type(S()), a.scales, a.m, a.groups, a.ldm * (int64_t)sizeof(S), 128, St::kGroups, false,
+    st = encode_map_2d(&sm, map_type(S()), a.scales, a.m, a.groups, a.ldm * (int64_t)sizeof(S), kRows, St::kGroups, false,
                        "scales");
     if (st != LRC_OK) return st;
     if (ZEROS) {
-        st = encode_map_2d(&zm, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.zeros, a.m, a.groups, a.ldm, 128, St::kGroups, false,
+        st = encode_map_2d(&zm, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.zeros, a.m, a.groups, a.ldm, kRows, St::kGroups, false,
                            "zeros");
         if (st != LRC_OK) return st;
     }
     auto kernel = q4_wide_kernel<OP, S, PARTS, GROUP, ZEROS, NC>;
-    constexpr int kSmem = St::kDepth * St::kPitch + 1024;
+    constexpr int kSmem = kPairs * St::kDepth * St::kPitch + 1024;
     // the attribute is the device's: set once on each
     static std::atomic<uint64_t> set_on{0};
     int dev = 0;
