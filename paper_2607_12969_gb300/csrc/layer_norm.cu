@@ -281,6 +281,271 @@ __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : sizeof(X) == 2 ? 
     }
 }
 
+// Where the rows of a tensor start within 16 bytes: their copies keep it, so that
+// whole 16 bytes of a row go by one bulk copy and its first and last elements by
+// plain loads.  Nothing beside the row is read.
+template <typename T>
+struct Span {
+    uint32_t head, body, mis;                // elements before and within the bulk copy; bytes past a boundary
+    __device__ Span(const T* row, int64_t cols) {
+        constexpr uint32_t kPer = 16 / sizeof(T);
+        mis = (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u);
+        head = min((uint32_t)cols, ((16u - mis) & 15u) / (uint32_t)sizeof(T));
+        body = ((uint32_t)cols - head) / kPer * kPer;
+    }
+};
+
+constexpr int kMostRing = 8;                 // rows of a ring
+constexpr int kRing = 225 * 1024;            // bytes of the rings of a multiprocessor
+constexpr int kStreamThreads = 1024;         // of a block, at most
+constexpr int kMostTeams = 15;               // of a block: a named barrier each
+
+// s / n with `inv` next to 1 / n (0 for no elements): the product, and its remainder's.
+__device__ __forceinline__ float quotient(float s, float n, float inv) {
+    const float near = s * inv;
+    return isinf(near) ? near : fmaf(fmaf(-near, n, s), inv, near);
+}
+
+// x^(-1/2): the approximation after one Newton step.
+__device__ __forceinline__ float reciprocal_root(float x) {
+    const float r = rsqrtf(x), s = fmaf(0.5f * r, fmaf(-x * r, r, 1.f), r);
+    return x > 0.f && x < __int_as_float(0x7f800000) ? s : r;        // not for 0 and infinity
+}
+
+// Many rows: a block's teams of blockDim.x threads (blockDim.y of them) take every
+// (number of teams)-th row each, in a ring in shared memory that bulk copies fill
+// rows ahead; gamma and beta are there too, in binary32, for all teams.  A row is in
+// registers between its sums and its result, and its place is free at its one
+// barrier; the sums as in norm_kernel.  VEC: every row starts on a 16-byte boundary,
+// eight columns side by side a thread; else a warp's columns are side by side, and
+// the result passes through shared memory, from where its whole 16 bytes go by one
+// bulk copy.  EDGES: x has elements outside the bulk copies, which the team's first
+// warp loads when it asks for the copies and puts beside them a row later.
+// What bounds it (8192 x 8192 of bfloat16, 55 us, 4.9 TB/s of 6.8): a quarter of the
+// warp's instructions wait for shared memory, whose pipe is 60 % busy, two thirds of
+// that with gamma and beta; 2.5 instructions a cycle.  Blocks that keep them apart
+// in every block (two a multiprocessor) have room for fewer rows: 62 us.
+template <typename X, typename Y, bool VEC, bool EDGES, int G>
+__global__ void __launch_bounds__(kStreamThreads, 1)
+norm_stream_kernel(const __grid_constant__ NormArgs a, const int depth) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ float sums[2][2][32];         // [parity][sum][warp]
+    __shared__ uint64_t all_full[kMostTeams][kMostRing];
+    __shared__ int abort_flag;
+    const int T = blockDim.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cols = (int)a.cols;
+    const X* x = static_cast<const X*>(a.x);
+    const int team = threadIdx.y, first = blockIdx.x * blockDim.y + team, teams = gridDim.x * blockDim.y;
+    const int mine = first < a.rows ? (int)((a.rows - first + teams - 1) / teams) : 0;
+    uint64_t* full = all_full[team];
+    const uint32_t pitch = ((uint32_t)(cols * sizeof(X)) + 31) & ~15u;
+    const uint32_t stage_pitch = VEC ? 0 : ((uint32_t)(cols * sizeof(Y)) + 31) & ~15u;
+    volatile int* abort = &abort_flag;
+    if (threadIdx.x == 0) {
+        if (team == 0) abort_flag = 0;
+        for (int d = 0; d < depth; ++d) tc::mbar_init(&full[d], EDGES ? 2 : 1);
+        tc::fence_barrier_init();
+    }
+    __syncthreads();
+    tc::pdl_wait();
+    tc::pdl_trigger();
+
+    float* gamma = reinterpret_cast<float*>(smem);
+    float* beta = gamma + T * 8 * G;
+    uint8_t* stage = reinterpret_cast<uint8_t*>(beta + T * 8 * G) + team * (depth * pitch + stage_pitch);
+    uint8_t* ring = stage + stage_pitch;
+    int edge_at = -1;                        // where this lane's element goes, -1 for none
+    X edge = el::from_f32<X>(0.f);
+    auto issue = [&](int k, int slot) {      // warp 0 (without edges, its first thread)
+        const X* xr = x + (first + (int64_t)k * teams) * a.ldx;
+        uint8_t* to = ring + slot * pitch;
+        if (!EDGES) {
+            tc::mbar_arrive_expect_tx(&full[slot], cols * (uint32_t)sizeof(X));
+            tc::bulk_load(to, xr, cols * (uint32_t)sizeof(X), &full[slot]);
+            return;
+        }
+        const Span<X> sx(xr, cols);
+        if (lane == 0) {
+            const uint32_t bytes = sx.body * sizeof(X);
+            tc::mbar_arrive_expect_tx(&full[slot], bytes);
+            if (bytes) tc::bulk_load(to + sx.mis + sx.head * sizeof(X), xr + sx.head, bytes, &full[slot]);
+        }
+        // lanes 0 ... 7 have the elements before the bulk copy, 8 ... 15 those after it
+        const bool after = lane & 8;
+        const uint32_t i = (lane & 7) + (after ? sx.head + sx.body : 0);
+        edge_at = -1;
+        if (lane < 16 && i < (after ? (uint32_t)cols : sx.head)) {
+            edge_at = (int)(slot * pitch + sx.mis + i * sizeof(X));
+            edge = xr[i];
+        }
+    };
+    auto put_edges = [&](int slot) {         // warp 0: of the row last asked for
+        if (edge_at >= 0) *reinterpret_cast<X*>(ring + edge_at) = edge;
+        tc::fence_proxy_async_smem();        // a later copy may write there
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&full[slot]);
+    };
+    int issued = 0;
+    if (EDGES ? warp == 0 : threadIdx.x == 0)
+        for (; issued < depth && issued < mine; ++issued) {
+            if (EDGES && issued) put_edges(issued - 1);
+            issue(issued, issued);
+        }
+    // (VEC: the first four columns of every thread side by side, then the others; else
+    // gamma and beta of a column side by side)
+    for (int c = team * T + threadIdx.x; c < cols; c += T * blockDim.y) {
+        const int at = VEC ? ((c / (8 * T) * 2 + (c >> 2 & 1)) * T + (c >> 3) % T) * 4 + (c & 3) : 2 * c;
+        gamma[at] = a.gamma ? el::load_as(a.gamma, a.pk, c) : 1.f;
+        (VEC ? beta : gamma + 1)[at] = a.beta ? el::load_as(a.beta, a.pk, c) : 0.f;
+    }
+    if (EDGES && warp == 0 && issued) put_edges(issued - 1);
+    __syncthreads();
+
+    const int step = VEC ? 1 : T;
+    auto column = [&](int k) { return VEC ? (k * T + (int)threadIdx.x) * 8 : k * T * 8 + (int)threadIdx.x; };
+    // numbers of elements of this warp and of warp `lane`
+    auto elements = [&](int w) {
+        int n = 0;
+        if (VEC) {
+            for (int k = 0; k < G; ++k) n += min(max(cols - (k * T + w * 32) * 8, 0), 256);
+        } else {
+            for (int k = 0; k < G * 8; ++k) n += min(max(cols - k * T - w * 32, 0), 32);
+        }
+        return (float)n;
+    };
+    const int warps = T >> 5, warp0 = team * warps;
+    const float n = elements(warp), inv = n > 0.f ? 1.f / n : 0.f;
+    const float inv_cols = 1.f / (float)a.cols;
+    const float n_l = lane < warps ? elements(lane) : 0.f, inv_l = n_l > 0.f ? 1.f / n_l : 0.f;
+    int slot = 0, p = 0, waiting = -1;       // waiting: place whose edges are not there yet
+    uint32_t phase = 0;
+    for (int k = 0; k < mine; ++k) {
+        const int64_t row = first + (int64_t)k * teams;
+        // after a wait that gave up the rows go on without copies or waits
+        tc::mbar_wait(&full[slot], phase, abort, &g_err_norm, 1u);
+        const X* at = reinterpret_cast<const X*>(ring + slot * pitch + (VEC ? 0 : (reinterpret_cast<uintptr_t>(x + row * a.ldx) & 15u)));
+        f2 v[G][4], s2 = 0, q2 = 0;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            float w[8];
+            if (!VEC && column(g) + 7 * T < cols) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = el::to_f32(at[column(g) + e * T]);
+            } else {
+                load_row<VEC>(at, column(g), T, cols, 0.f, w);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[g][e] = pair(w[2 * e], w[2 * e + 1]);
+                s2 = add2(s2, v[g][e]);
+            }
+        }
+        const float s = el::warp_sum(both_of(s2)), m = quotient(s, n, inv);
+        const f2 m2 = pair(-m, -m);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const int c = column(g);
+            if (c + 7 * step < cols) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f2 d = add2(v[g][e], m2);
+                    q2 = fma2(d, d, q2);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float d0, d1;
+                    split(add2(v[g][e], m2), d0, d1);
+                    const f2 d = pair(c + 2 * e * step < cols ? d0 : 0.f, c + (2 * e + 1) * step < cols ? d1 : 0.f);
+                    q2 = fma2(d, d, q2);
+                }
+            }
+        }
+        const float q = el::warp_sum(both_of(q2));
+        if (lane == 0) sums[p][0][warp0 + warp] = s, sums[p][1][warp0 + warp] = q;
+        if (!VEC && threadIdx.x == 0) tc::bulk_wait_read<0>();       // the last result has left `stage`
+        tc::named_bar_sync(1 + team, T);     // every warp has the row in registers
+        if (EDGES ? warp == 0 : threadIdx.x == 0) {
+            if (EDGES && waiting >= 0) put_edges(waiting);
+            waiting = -1;
+            if (issued < mine && !*abort) {
+                issue(issued, slot);
+                ++issued;
+                waiting = slot;
+            }
+        }
+        if (++slot == depth) {
+            slot = 0;
+            phase ^= 1;
+        }
+        const float sw = lane < warps ? sums[p][0][warp0 + lane] : 0.f, qw = lane < warps ? sums[p][1][warp0 + lane] : 0.f;
+        p ^= 1;
+        float mu = sw;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) mu += __shfl_xor_sync(0xffffffffu, mu, o);
+        mu = quotient(mu, (float)a.cols, inv_cols);
+        const float d = n_l > 0.f ? quotient(sw, n_l, inv_l) - mu : 0.f;
+        float var = fmaf(n_l * d, d, qw);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) var += __shfl_xor_sync(0xffffffffu, var, o);
+        const float r = reciprocal_root(fmaf(var, inv_cols, a.eps));
+        if (threadIdx.x == 0) {
+            if (a.mean) a.mean[row] = mu;
+            if (a.rstd) a.rstd[row] = r;
+        }
+        Y* y = static_cast<Y*>(a.y) + row * a.ldy;
+        const f2 mu2 = pair(-mu, -mu), r2 = pair(r, r);
+        const Span<Y> sy(y, cols);
+        Y* out = reinterpret_cast<Y*>(stage + sy.mis);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const int c = column(g);
+            float w[8], b[8], u[8];
+            if (VEC) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int i = (g * 2 + h) * T + (int)threadIdx.x;
+                    const float4 wv = reinterpret_cast<const float4*>(gamma)[i], bv = reinterpret_cast<const float4*>(beta)[i];
+                    w[4 * h] = wv.x, w[4 * h + 1] = wv.y, w[4 * h + 2] = wv.z, w[4 * h + 3] = wv.w;
+                    b[4 * h] = bv.x, b[4 * h + 1] = bv.y, b[4 * h + 2] = bv.z, b[4 * h + 3] = bv.w;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float2 wb = reinterpret_cast<const float2*>(gamma)[c + e * T];
+                    w[e] = wb.x, b[e] = wb.y;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                split(fma2(mul2(add2(v[g][e], mu2), r2), pair(w[2 * e], w[2 * e + 1]), pair(b[2 * e], b[2 * e + 1])), u[2 * e], u[2 * e + 1]);
+            if (VEC) store_row<true>(y, c, T, cols, u);
+            else if (c + 7 * T < cols) store_row<false>(out, c, T, 0x7fffffff, u);
+            else store_row<false>(out, c, T, cols, u);
+        }
+        if (!VEC) {
+            tc::fence_proxy_async_smem();
+            tc::named_bar_sync(1 + team, T);
+            if (threadIdx.x == 0 && sy.body) {
+                tc::bulk_store(y + sy.head, out + sy.head, sy.body * (uint32_t)sizeof(Y));
+                tc::bulk_commit();
+            }
+            if (threadIdx.x >= T - 16) {     // the elements before (at most seven) and after that copy
+                const uint32_t e = threadIdx.x & 15, i = e < 8 ? e : sy.head + sy.body + e - 8;
+                if (i < (e < 8 ? sy.head : (uint32_t)cols)) y[i] = out[i];
+            }
+        }
+    }
+    if (!VEC && threadIdx.x == 0) tc::bulk_wait<0>();
+    if (warp == 0 && *abort) {
+        // the copies in flight end before the block does
+        if (EDGES && waiting >= 0) put_edges(waiting);
+        volatile int no_abort = 0;
+        if (lane == 0)
+            for (int u = issued > depth ? issued - depth : 0; u < issued; ++u)
+                tc::mbar_wait(&full[u % depth], u / depth & 1, &no_abort, &g_err_norm, 1u, 100000000ull);
+    }
+}
+
 // Rows too long for the registers of a block: read three times (from L2 after the
 // first).
 template <typename X, typename Y>
@@ -325,21 +590,6 @@ struct GradArgs {
     int pk;
 };
 
-// Where the rows of a tensor start within 16 bytes: their copies keep it, so that
-// whole 16 bytes of a row go by one bulk copy and its first and last elements by
-// plain loads.  Nothing beside the row is read.
-template <typename T>
-struct Span {
-    uint32_t head, body, mis;                // elements before and within the bulk copy; bytes past a boundary
-    __device__ Span(const T* row, int64_t cols) {
-        constexpr uint32_t kPer = 16 / sizeof(T);
-        mis = (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u);
-        head = min((uint32_t)cols, ((16u - mis) & 15u) / (uint32_t)sizeof(T));
-        body = ((uint32_t)cols - head) / kPer * kPer;
-    }
-};
-
-constexpr int kMostRing = 8;                 // rows of a ring
 constexpr int kGradThreads = 512;            // of a block, at most
 
 // A cluster takes every (number of clusters)-th row, each of its blocks a slice of
@@ -366,7 +616,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_kernel(const __grid
     const int cols = (int)min(a.slice, a.cols - c0);                       // this block's columns
     const X* x = static_cast<const X*>(a.x) + c0;
     const Y* dy = static_cast<const Y*>(a.dy) + c0;
-    const int mine = first < a.rows ? ((int)a.rows - first + clusters - 1) / clusters : 0;
+    const int mine = first < a.rows ? (int)((a.rows - first + clusters - 1) / clusters) : 0;
     const uint32_t ypart = (uint32_t)(a.slice * sizeof(X) + 16), pitch = ypart + (uint32_t)(a.slice * sizeof(Y) + 16);
     volatile int* abort = &abort_flag;
     if (threadIdx.x == 0) {
@@ -421,6 +671,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_kernel(const __grid
             if (lane >= 16) *reinterpret_cast<Y*>(ring + edge_at) = ye;
             else *reinterpret_cast<X*>(ring + edge_at) = xe;
         }
+        tc::fence_proxy_async_smem();        // a later copy may write there
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&full[slot]);
     };
@@ -672,6 +923,46 @@ lrc_status norm_as(const NormArgs& a, cudaStream_t s) {
     // Many rows: 256 threads a row or fewer, so that a multiprocessor has several rows
     // at different points of their chain; few rows: eight values a thread.
     const bool many = a.rows >= 2 * (int64_t)sm_count();
+    // Rows enough to pay for bringing gamma and beta to every multiprocessor, long
+    // enough for a few warps: norm_stream_kernel against norm_kernel, bfloat16, us.
+    //   8192 x 8192: 55, 75.  4096: 31, 40.  2048: 21, 24.  1024: 19, 13.
+    //   8191 x 4097: 46, 107.  1025: 22, 29.  513: 15, 18.
+    //   2600 x 8192: 26, 30.  1300: 20.4, 20.2.  700: 12.0, 9.9.
+    //   700 x 4097: 10, 20.  1025: 7.8, 6.9.
+    if (a.rows >= (vec ? 16 : 4) * (int64_t)sm_count() && groups <= 2048 && groups > (vec ? 128 : 64)) {
+        const int pitch = ((int)(a.cols * (int64_t)sizeof(X)) + 31) & ~15;
+        const int stage = vec ? 0 : ((int)(a.cols * (int64_t)sizeof(Y)) + 31) & ~15;
+        // 32 columns a thread (a warp's sums and its row's ends are half of its
+        // instructions) where the teams that fit, two rows in the ring each, fill a
+        // block; else 16: 8192 x 8192 of binary32 (two teams of 256 threads, or of 512)
+        // is 7 % slower with 32, of bfloat16 9 % faster; 8191 x 1025 24 us and 22.
+        int G = 4, teams = 0, depth = 0, params = 0;
+        unsigned T = 0;
+        for (; G >= 2; G /= 2) {
+            T = (unsigned)((groups + 32 * G - 1) / (32 * G) * 32);
+            params = (int)T * 8 * G * 8;
+            teams = T < 64 ? kMostTeams : (int)(1024 / T) < kMostTeams ? (int)(1024 / T) : kMostTeams;
+            const int room = kRing - params;
+            while (teams && room / teams < stage + 2 * pitch) --teams;
+            depth = teams ? (room / teams - stage) / pitch : 0;
+            if (groups > 256 && teams * T >= 768) break;
+        }
+        if (G < 2) G = 2;
+        if (depth > kMostRing) depth = kMostRing;
+        if (teams) {
+            auto pick = [&](auto g) {
+                constexpr int kG = decltype(g)::value;
+                return !vec ? norm_stream_kernel<X, Y, false, true, kG>
+                            : a.cols % 8 ? norm_stream_kernel<X, Y, true, true, kG> : norm_stream_kernel<X, Y, true, false, kG>;
+            };
+            auto kernel = G == 2 ? pick(std::integral_constant<int, 2>()) : pick(std::integral_constant<int, 4>());
+            cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing);
+            if (e != cudaSuccess) return cuda_fail(e, "norm_stream_kernel");
+            e = launch_pdl(kernel, dim3((unsigned)sm_count()), dim3(T, (unsigned)teams), (size_t)(teams * (depth * pitch + stage) + params), s, a, depth);
+            if (e != cudaSuccess) return cuda_fail(e, "norm_stream_kernel");
+            return after_launch("norm_stream_kernel");
+        }
+    }
     if (many && groups <= 1024) {
         if (groups <= 256) return vec ? go(norm_kernel<X, Y, true, 1, 256>, 1) : go(norm_kernel<X, Y, false, 1, 256>, 1);
         if (groups <= 512) return vec ? go(norm_kernel<X, Y, true, 2, 256>, 2) : go(norm_kernel<X, Y, false, 2, 256>, 2);
@@ -687,7 +978,6 @@ lrc_status norm_as(const NormArgs& a, cudaStream_t s) {
 
 // Columns of a block at most, blocks of a cluster at most, bytes of its ring.
 constexpr int64_t kSlice = 8192;
-constexpr int kRing = 225 * 1024;
 
 template <typename X, typename Y>
 lrc_status norm_grad_as(GradArgs a, float* dgamma, float* dbeta, cudaStream_t s) {

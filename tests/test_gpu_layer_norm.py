@@ -60,6 +60,42 @@ def test_norm(lrc, cuda, rows, cols, fmt, pfmt, pad, shift):
     R.frame_kept(y, yb)
 
 
+# Many rows, enough for blocks that keep going from row to row.
+MANY = [(2432, 1025), (2500, 1100), (2433, 2048), (2440, 2050), (2600, 4104), (2437, 8192), (2435, 8190), (2441, 12296),
+        (2433, 16384), (611, 513), (700, 1025), (609, 4097), (608, 9001), (608, 16383)]
+
+
+@pytest.mark.parametrize("rows,cols", MANY)
+@pytest.mark.parametrize("fmt,pfmt", [("f32", "f32"), ("f16", "f16"), ("f16_o16", "f32"), ("bf16", "bf16"), ("bf16", None)])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (5, 1)])
+def test_norm_of_many_rows(lrc, cuda, rows, cols, fmt, pfmt, pad, shift):
+    test_norm(lrc, cuda, rows, cols, fmt, pfmt, pad, shift)
+
+
+@pytest.mark.parametrize("rows,cols,shift", [(2500, 4096, 0), (2500, 2050, 0), (700, 2049, 3)])
+def test_many_rows_in_place_far_from_zero_and_not_finite(lrc, cuda, rows, cols, shift):
+    x, gamma, beta, _ = inputs(cuda, rows, cols, "f32", "f32", 7, cols + shift, shift)
+    x += 1e4
+    x[5] = 3.0                                  # (equal values: x - mu is 0)
+    y, mean, rstd = torch.empty(rows, cols, device=cuda), torch.empty(rows, device=cuda), torch.empty(rows, device=cuda)
+    lrc.lrc_layer_norm(x, gamma, beta, y, mean, rstd, rows, cols, cols + shift, cols, 1e-5, "f32", "f32")
+    want = R.layer_norm(x, gamma, beta, 1e-5)
+    by, bm, br = norm_bounds(x, gamma, beta, want, 1e-5, torch.float32)
+    keep = torch.arange(rows, device=cuda) != 5
+    R.within(y[keep], want[0][keep], by[keep], "y")
+    R.within(mean, want[1], bm, "mean")
+    R.within(rstd[keep], want[2][keep], br[keep], "rstd")
+    assert torch.equal(y[5], beta.float()) and mean[5].item() == 3.0
+    x[9, 2], x[11, cols - 1] = float("nan"), float("inf")
+    lrc.lrc_layer_norm(x, gamma, beta, x, None, None, rows, cols, cols + shift, cols + shift, 1e-5, "f32", "f32")
+    bad = torch.zeros(rows, dtype=torch.bool, device=cuda)
+    bad[9] = bad[11] = True
+    assert x[bad].isnan().all() and torch.equal(x[~bad], y[~bad])
+    x[3] = 2.0
+    lrc.lrc_layer_norm(x, gamma, beta, x, None, rstd, rows, cols, cols + shift, cols + shift, 0.0, "f32", "f32")
+    assert x[3].isnan().all() and rstd[3].item() == float("inf")
+
+
 def test_norm_of_rows_far_from_zero(lrc, cuda):
     """A mean 10^4 standard deviations away: the squares are of x - mu."""
     rows, cols = 6, 3000
