@@ -1,6 +1,5 @@
-// q4.cu -- matrices of 4-bit codes with a scale per row and group of columns:
-// rounding, widening, and the product with a few vectors (lrc_q4_round,
-// lrc_q4_widen, lrc_q4_apply).
+// q4.cu -- the product of a matrix of 4-bit codes with vectors (lrc_q4_apply): the
+// kernel for up to 32 columns of them, and the choice.
 //
 // What[i][c] = s (q - z).  The codes' layout is the one include/lrc.h states:
 // 64-byte blocks of 128 columns, column 32 j + 8 t + e in word 4 t + j.
@@ -14,192 +13,6 @@ namespace lrc {
 namespace {
 
 using namespace q4;
-
-constexpr float kSeventh = 0.14285714285714285f;      // binary32 next to 1/7
-constexpr float kFifteenth = 0.06666666666666667f;    // and to 1/15
-
-// Bit position of column e of a word.
-__device__ __forceinline__ int nibble_shift(int e) { return 2 * e + (e & 1) * 14; }
-
-template <typename S> __device__ __forceinline__ float largest();
-template <> __device__ __forceinline__ float largest<float>() { return 3.402823466e38f; }
-template <> __device__ __forceinline__ float largest<__half>() { return 65504.f; }
-template <> __device__ __forceinline__ float largest<bf16>() { return 3.3895313892515355e38f; }
-
-__device__ __forceinline__ float src_f32(double x) { return (float)x; }
-template <typename T> __device__ __forceinline__ float src_f32(T x) { return el::to_f32(x); }
-
-// Rounding and widening go over pieces of kPieceRows rows and 256 columns, a block
-// each; a warp takes every eighth row.  The scales of a piece pass through shared
-// memory: in memory the rows are side by side, not the groups.
-constexpr int kPieceRows = 32, kPieceCols = 256;
-
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float d;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-    return d;
-}
-__device__ __forceinline__ float min_nan(float a, float b) {
-    float d;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-    return d;
-}
-
-// Eight elements of a row from column c on, zeros from n on.
-template <typename W>
-__device__ __forceinline__ void load_columns(const W* row, int64_t c, int64_t n, bool whole16, float (&w)[8]) {
-    if (whole16 && c + 8 <= n) {
-        constexpr int kLoads = (int)sizeof(W) * 8 / 16;
-        union {
-            uint4 q[kLoads];
-            W e[8];
-        } u;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) u.q[i] = __ldcs(reinterpret_cast<const uint4*>(row + c) + i);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = src_f32(u.e[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = c + e < n ? src_f32(row[c + e]) : 0.f;
-    }
-}
-
-// A thread rounds eight consecutive columns, a word of codes; group / 8 neighbouring
-// lanes share a scale.  Adding 1.5 * 2^23 rounds to an integer, ties to even, and
-// leaves it in the low bits; the word is the sum of those, each times its power of
-// 16 (on the multipliers' pipe), less what the eight constants add.  Bound by
-// instructions: 16384 x 8192 of bfloat16 with zero codes 97 us, 3.5 TB/s.
-template <typename W, typename S, int GROUP, bool ZEROS>
-__global__ void __launch_bounds__(256)
-q4_round_kernel(const W* __restrict__ src, int64_t m, int64_t n, int64_t ldw, bool whole16, uint32_t* __restrict__ Q,
-                S* __restrict__ scales, uint8_t* __restrict__ zeros, int64_t blocks, int64_t pieces, int64_t ldm) {
-    constexpr int kGroups = kPieceCols / GROUP, kLanes = GROUP / 8;
-    __shared__ S sh_s[kGroups][kPieceRows];
-    __shared__ uint8_t sh_z[kGroups][kPieceRows];
-    const int64_t r0 = blockIdx.x / pieces * kPieceRows, piece = blockIdx.x % pieces;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t c0 = piece * kPieceCols + lane * 8;
-    const int chunk = lane & 15;                             // of the block of 128 columns: 4 j + t
-    const int64_t word_at = (piece * 2 + (lane >> 4)) * 16 + (chunk & 3) * 4 + (chunk >> 2);
-    tc::pdl_wait();
-    tc::pdl_trigger();
-#pragma unroll
-    for (int i = 0; i < kPieceRows / 8; ++i) {
-        const int r = warp + 8 * i;
-        const int64_t row = r0 + r;
-        if (row >= m) break;
-        float w[8];
-        load_columns(src + row * ldw, c0, n, whole16, w);
-        float lo = 0.f, hi = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (ZEROS) {
-                lo = min_nan(lo, w[e]);
-                hi = max_nan(hi, w[e]);
-            } else {
-                hi = max_nan(hi, fabsf(w[e]));
-            }
-        }
-#pragma unroll
-        for (int o = 1; o < kLanes; o <<= 1) {
-            if (ZEROS) lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-            hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-        }
-        const bool bad = !(hi <= 3.402823466e38f) || !(lo >= -3.402823466e38f);
-        const float wide = ZEROS ? __fmul_rn(__fsub_rn(hi, lo), kFifteenth) : __fmul_rn(hi, kSeventh);
-        S stored = el::from_f32<S>(fminf(wide, largest<S>()));
-        const float s = el::to_f32(stored);
-        const bool none = s < 1.17549435e-38f;
-        const float inv = none ? 0.f : __frcp_rn(s);
-        if (none) stored = el::from_f32<S>(0.f);
-        float z = 8.f;
-        if (ZEROS) z = fminf(fmaxf(rintf(__fmul_rn(-lo, inv)), 0.f), 15.f);
-        if (bad) {
-            stored = el::from_f32<S>(__int_as_float(0x7fffffff));
-            z = 8.f;
-        }
-        constexpr uint32_t kBits = 0x4b400000u;              // of 1.5 * 2^23
-        uint32_t word = ((uint32_t)(int)z - kBits) * 0x11111111u;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float v = fminf(fmaxf(__fmul_rn(w[e], inv), -z), 15.f - z);
-            word += __float_as_uint(__fadd_rn(v, 12582912.f)) << nibble_shift(e);
-        }
-        if (bad) word = 0x88888888u;
-        if ((piece * 2 + (lane >> 4)) < blocks) Q[row * blocks * 16 + word_at] = word;
-        if (lane % kLanes == 0) {
-            sh_s[lane / kLanes][r] = stored;
-            if (ZEROS) sh_z[lane / kLanes][r] = (uint8_t)(int)z;
-        }
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < kGroups * kPieceRows; e += 256) {
-        const int64_t g = piece * kGroups + e / kPieceRows, row = r0 + e % kPieceRows;
-        if (g * GROUP < n && row < m) {
-            scales[g * ldm + row] = sh_s[e / kPieceRows][e % kPieceRows];
-            if (ZEROS) zeros[g * ldm + row] = sh_z[e / kPieceRows][e % kPieceRows];
-        }
-    }
-}
-
-template <typename D> __device__ __forceinline__ D wide(float s, int q) { return el::from_f32<D>(__fmul_rn(s, (float)q)); }
-template <> __device__ __forceinline__ double wide<double>(float s, int q) { return (double)s * (double)q; }
-
-// Widening, VEC columns a lane at a time: 16 bytes, or one element where the rows of
-// dst start anywhere.  16384 x 8192 to binary32 with zero codes, bound by the writes:
-// 92 us, 6.6 TB/s.
-template <typename S, typename D, int VEC>
-__global__ void __launch_bounds__(256)
-q4_widen_kernel(const uint32_t* __restrict__ Q, const S* __restrict__ scales, const uint8_t* __restrict__ zeros,
-                int group, int64_t m, int64_t n, int64_t blocks, int64_t pieces, int64_t ldm, D* __restrict__ dst,
-                int64_t ld) {
-    __shared__ float sh_s[kPieceCols / 32][kPieceRows];
-    __shared__ int sh_z[kPieceCols / 32][kPieceRows];
-    const int64_t r0 = blockIdx.x / pieces * kPieceRows, piece = blockIdx.x % pieces;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, groups = kPieceCols / group;
-    tc::pdl_wait();
-    tc::pdl_trigger();
-    for (int e = threadIdx.x; e < groups * kPieceRows; e += 256) {
-        const int64_t g = piece * groups + e / kPieceRows, row = r0 + e % kPieceRows;
-        if (g * group < n && row < m) {
-            sh_s[e / kPieceRows][e % kPieceRows] = el::to_f32(scales[g * ldm + row]);
-            sh_z[e / kPieceRows][e % kPieceRows] = zeros ? (int)zeros[g * ldm + row] : 8;
-        }
-    }
-    __syncthreads();
-    const int shift_of_group = group == 32 ? 5 : group == 64 ? 6 : 7;
-#pragma unroll
-    for (int i = 0; i < kPieceRows / 8; ++i) {
-        const int r = warp + 8 * i;
-        const int64_t row = r0 + r;
-        if (row >= m) break;
-#pragma unroll
-        for (int k = 0; k < kPieceCols / (32 * VEC); ++k) {
-            const int cp = k * 32 * VEC + lane * VEC;        // column of the piece
-            const int64_t c = piece * kPieceCols + cp;
-            if (c >= n) continue;
-            const int chunk = (cp & 127) >> 3;
-            const uint32_t word =
-                __ldg(Q + (row * blocks + piece * 2 + (cp >> 7)) * 16 + (chunk & 3) * 4 + (chunk >> 2));
-            const float s = sh_s[cp >> shift_of_group][r];
-            const int z = sh_z[cp >> shift_of_group][r];
-            union {
-                uint4 q;
-                D e[VEC];
-            } u;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) u.e[e] = wide<D>(s, (int)((word >> nibble_shift((cp & 7) + e)) & 15u) - z);
-            D* to = dst + row * ld + c;
-            if (VEC > 1 && c + VEC <= n) {
-                __stcs(reinterpret_cast<uint4*>(to), u.q);
-            } else {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (c + e < n) to[e] = u.e[e];
-            }
-        }
-    }
-}
 
 // ---- product ---------------------------------------------------------------
 //
@@ -406,59 +219,6 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     if (a.split > 1) cl::sync();                              // the sums stay until they are read
 }
 
-lrc_status grid_of(int64_t threads, int per, const char* what, unsigned* out) {
-    const int64_t g = (threads + per - 1) / per;
-    if (g > 0x7fffffff) {
-        set_error("%s: too large for one launch", what);
-        return LRC_ERR_UNSUPPORTED;
-    }
-    *out = (unsigned)g;
-    return LRC_OK;
-}
-
-lrc_status pieces_of(int64_t m, int64_t n, const char* what, int64_t* pieces, unsigned* grid) {
-    *pieces = (n + kPieceCols - 1) / kPieceCols;
-    return grid_of((m + kPieceRows - 1) / kPieceRows * *pieces, 1, what, grid);
-}
-
-template <typename W, typename S>
-lrc_status round_as(const void* src, int64_t m, int64_t n, int64_t ldw, void* Q, void* scales, uint8_t* zeros, int group,
-                    cudaStream_t s) {
-    int64_t pieces;
-    unsigned grid;
-    lrc_status st = pieces_of(m, n, "lrc_q4_round", &pieces, &grid);
-    if (st != LRC_OK) return st;
-    const bool whole16 = aligned16(src) && ldw * (int64_t)sizeof(W) % 16 == 0;
-    auto go = [&](auto kernel) -> lrc_status {
-        const cudaError_t e = launch_pdl(kernel, dim3(grid), dim3(256), 0, s, (const W*)src, m, n, ldw, whole16,
-                                         (uint32_t*)Q, (S*)scales, zeros, (n + 127) / 128, pieces, lrc_packed_ld(m));
-        if (e != cudaSuccess) return cuda_fail(e, "q4_round_kernel");
-        return after_launch("q4_round_kernel");
-    };
-    if (zeros)
-        return group == 32 ? go(q4_round_kernel<W, S, 32, true>) : group == 64 ? go(q4_round_kernel<W, S, 64, true>)
-                                                                             : go(q4_round_kernel<W, S, 128, true>);
-    return group == 32 ? go(q4_round_kernel<W, S, 32, false>) : group == 64 ? go(q4_round_kernel<W, S, 64, false>)
-                                                                           : go(q4_round_kernel<W, S, 128, false>);
-}
-
-template <typename S, typename D>
-lrc_status widen_as(const void* Q, const void* scales, const uint8_t* zeros, int group, int64_t m, int64_t n, void* dst,
-                    int64_t ld, cudaStream_t s) {
-    int64_t pieces;
-    unsigned grid;
-    lrc_status st = pieces_of(m, n, "lrc_q4_widen", &pieces, &grid);
-    if (st != LRC_OK) return st;
-    auto go = [&](auto kernel) -> lrc_status {
-        const cudaError_t e = launch_pdl(kernel, dim3(grid), dim3(256), 0, s, (const uint32_t*)Q, (const S*)scales, zeros,
-                                         group, m, n, (n + 127) / 128, pieces, lrc_packed_ld(m), (D*)dst, ld);
-        if (e != cudaSuccess) return cuda_fail(e, "q4_widen_kernel");
-        return after_launch("q4_widen_kernel");
-    };
-    if (aligned16(dst) && ld * (int64_t)sizeof(D) % 16 == 0) return go(q4_widen_kernel<S, D, 16 / (int)sizeof(D)>);
-    return go(q4_widen_kernel<S, D, 1>);
-}
-
 // binary32 vectors as three bfloat16 parts, x = hi + mid + lo exactly (each cut
 // off, not rounded, so that none overflows): rows 3 v, 3 v + 1, 3 v + 2 of
 // `blocks` whole blocks of columns, zeros from n on.  An infinity or NaN is in
@@ -637,36 +397,6 @@ lrc_status apply_as(const void* Q, const void* scales, const uint8_t* zeros, con
 }
 
 }  // namespace
-
-lrc_status launch_q4_round(const void* W, lrc_fmt wfmt, int64_t m, int64_t n, int64_t ldw, void* Q, void* scales,
-                           uint8_t* zeros, int group, lrc_fmt fmt, cudaStream_t s) {
-    auto by_scale = [&](auto w) {
-        using WT = decltype(w);
-        if (fmt == LRC_F32) return round_as<WT, float>(W, m, n, ldw, Q, scales, zeros, group, s);
-        if (fmt == LRC_BF16) return round_as<WT, bf16>(W, m, n, ldw, Q, scales, zeros, group, s);
-        return round_as<WT, __half>(W, m, n, ldw, Q, scales, zeros, group, s);
-    };
-    switch (wfmt) {
-        case LRC_F64: return by_scale(double());
-        case LRC_F32: return by_scale(float());
-        case LRC_BF16: return by_scale(bf16());
-        default: return by_scale(__half());
-    }
-}
-
-lrc_status launch_q4_widen(const void* Q, const void* scales, const uint8_t* zeros, int group, lrc_fmt fmt, int64_t m,
-                           int64_t n, void* dst, lrc_fmt dfmt, int64_t ld, cudaStream_t s) {
-    auto by_dst = [&](auto sc) {
-        using ST = decltype(sc);
-        if (dfmt == LRC_F64) return widen_as<ST, double>(Q, scales, zeros, group, m, n, dst, ld, s);
-        if (dfmt == LRC_F32) return widen_as<ST, float>(Q, scales, zeros, group, m, n, dst, ld, s);
-        if (dfmt == LRC_BF16) return widen_as<ST, bf16>(Q, scales, zeros, group, m, n, dst, ld, s);
-        return widen_as<ST, __half>(Q, scales, zeros, group, m, n, dst, ld, s);
-    };
-    if (fmt == LRC_F32) return by_dst(float());
-    if (fmt == LRC_BF16) return by_dst(bf16());
-    return by_dst(__half());
-}
 
 lrc_status launch_q4_apply(const void* Q, const void* scales, const uint8_t* zeros, const void* X, const void* A, void* Y,
                            int64_t m, int64_t n, int64_t b, int group, lrc_fmt fmt, cudaStream_t s) {

@@ -102,6 +102,16 @@ constexpr CUtensorMapDataType map_type(bf16) { return CU_TENSOR_MAP_DATA_TYPE_BF
 
 constexpr int kSmemOfSm = 227 * 1024;
 
+inline lrc_status grid_of(int64_t threads, int per, const char* what, unsigned* out) {
+    const int64_t g = (threads + per - 1) / per;
+    if (g > 0x7fffffff) {
+        set_error("%s: too large for one launch", what);
+        return LRC_ERR_UNSUPPORTED;
+    }
+    *out = (unsigned)g;
+    return LRC_OK;
+}
+
 // The end of a tile: sums of SETS sets (set s, column c, row r of the tile at sums[s *
 // set + c * pitch + r], pitch a multiple of four) and of the blocks of the cluster,
 // added in a fixed order, four rows a thread; then A and the rounding.  All loads of

@@ -72,6 +72,37 @@ def test_round_at_the_ends_of_the_ranges(lrc, cuda, zeros):
             assert np.array_equal(q.zeros[:, :m].cpu().numpy(), z), fmt
 
 
+@pytest.mark.parametrize("src", ["f16", "bf16"])
+@pytest.mark.parametrize("n", [24, 39, 130, 517, 1040])
+@pytest.mark.parametrize("pad", [0, 1, 6, 8])
+def test_round_of_16_bit_rows_that_start_anywhere(lrc, cuda, src, n, pad):
+    """Every place within 16 bytes; a NaN beside a row would show; the ends of
+    the ranges in groups of their own."""
+    inf, nan, m = float("inf"), float("nan"), 41
+    gen = torch.Generator(device=cuda).manual_seed(n + pad)
+    for shift in range(9):
+        W, _ = R.framed((m, n), STORE[src], cuda, n + pad, shift=shift)
+        W.copy_(torch.randn((m, n), generator=gen, device=cuda) * 0.05)
+        W[3] = 0.0
+        W[4] = -W[4].abs()
+        W[5] = W[5].abs()
+        W[6, n // 2], W[7, 0], W[8, n - 1], W[9, n // 3] = nan, inf, -inf, -nan
+        W[10] *= 2.0 ** -18                                   # binary16: subnormal
+        W[11, ::2], W[11, 1::2] = 6e4, -6e4
+        W[12] = -0.0
+        for group, zeros, fmt in ((32, True, "f32"), (64, False, "bf16"), (128, True, "f16")):
+            Q = torch.empty((m, lrc.lrc_q4_row_bytes(n)), dtype=torch.uint8, device=cuda)
+            ld, groups = lrc.lrc_packed_ld(m), -(-n // group)
+            scales = torch.empty((groups, ld), dtype=STORE[fmt], device=cuda)
+            zc = torch.empty((groups, ld), dtype=torch.uint8, device=cuda) if zeros else None
+            lrc.lrc_q4_round(W, src, m, n, n + pad, Q, scales, zc, group, fmt)
+            codes, s, z = rounded_by_definition(W, group, zeros, STORE[fmt])
+            assert np.array_equal(R.q4_unpack(Q, n).cpu().numpy(), codes)
+            assert np.array_equal(scales[:, :m].float().cpu().numpy(), s, equal_nan=True)
+            if zeros:
+                assert np.array_equal(zc[:, :m].cpu().numpy(), z)
+
+
 @pytest.mark.parametrize("m,n,ld", [(1, 1, 1), (9, 130, 131), (64, 512, 512), (31, 1001, 1001), (8, 257, 272)])
 @pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True)])
 @pytest.mark.parametrize("fmt,dfmt", [("f16", "f64"), ("bf16", "f32"), ("f32", "f32"), ("f16", "bf16"), ("bf16", "f16"),
