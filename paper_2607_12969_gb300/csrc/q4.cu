@@ -65,7 +65,7 @@ constexpr int kMostRows = 7;
 constexpr int kMostDepth = 8;      // stages of a ring
 
 // OP: the instructions' element type; S: the scales' type; PARTS: columns of B
-// that make one vector (3: a binary32 vector as hi + mid + lo in bfloat16).
+// that make one vector (3: a binary32 vector's parts in bfloat16).
 template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NT>
 __global__ void __launch_bounds__(64 * kMostRows + 32, 1)
 q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap xmap,
@@ -219,10 +219,14 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     if (a.split > 1) cl::sync();                              // the sums stay until they are read
 }
 
-// binary32 vectors as three bfloat16 parts, x = hi + mid + lo exactly (each cut
-// off, not rounded, so that none overflows): rows 3 v, 3 v + 1, 3 v + 2 of
-// `blocks` whole blocks of columns, zeros from n on.  An infinity or NaN is in
-// the first part alone.
+// binary32 vectors as three bfloat16 parts, x = hi + 2^-8 mid + 2^-16 lo (each cut
+// off, not rounded, so that none overflows): rows 3 v, 3 v + 1, 3 v + 2 of `blocks`
+// whole blocks of columns, zeros from n on.  The powers of two bring each part to hi's
+// size: what is left of x has 8 bits fewer each time and every binary32 number is a
+// multiple of 2^-149, so the parts are multiples of 2^-133, bfloat16's smallest number,
+// and hold all of x however small it is.  (Not brought up, the last bits of entries
+// below 2^-110 were lost, 1e-4 of one of 2^-120.)  finish_tile takes the powers off the
+// sums.  An infinity or NaN is in the first part alone.
 __global__ void __launch_bounds__(256)
 q4_parts_kernel(const float* __restrict__ x, int64_t n, int64_t ldn, int64_t ldp, uint16_t* __restrict__ parts) {
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -232,9 +236,9 @@ q4_parts_kernel(const float* __restrict__ x, int64_t n, int64_t ldn, int64_t ldp
     const float v = c < n ? x[(int64_t)blockIdx.y * ldn + c] : 0.f;
     const uint32_t hi = __float_as_uint(v) & 0xffff0000u;
     const bool odd = !(fabsf(v) <= 3.402823466e38f);
-    const float rest = odd ? 0.f : v - __uint_as_float(hi);
+    const float rest = odd ? 0.f : (v - __uint_as_float(hi)) * kPartUp;
     const uint32_t mid = __float_as_uint(rest) & 0xffff0000u;
-    const float last = rest - __uint_as_float(mid);
+    const float last = (rest - __uint_as_float(mid)) * kPartUp;
     uint16_t* p = parts + (int64_t)blockIdx.y * 3 * ldp + c;
     p[0] = odd && v != v ? 0x7fffu : (uint16_t)(hi >> 16);
     p[ldp] = (uint16_t)(mid >> 16);

@@ -102,6 +102,9 @@ constexpr CUtensorMapDataType map_type(bf16) { return CU_TENSOR_MAP_DATA_TYPE_BF
 
 constexpr int kSmemOfSm = 227 * 1024;
 
+// Each part of a binary32 vector after the first is 2^8 times what is left of it.
+constexpr float kPartUp = 256.f;
+
 inline lrc_status grid_of(int64_t threads, int per, const char* what, unsigned* out) {
     const int64_t g = (threads + per - 1) / per;
     if (g > 0x7fffffff) {
@@ -114,7 +117,8 @@ inline lrc_status grid_of(int64_t threads, int per, const char* what, unsigned* 
 
 // The end of a tile: sums of SETS sets (set s, column c, row r of the tile at sums[s *
 // set + c * pitch + r], pitch a multiple of four) and of the blocks of the cluster,
-// added in a fixed order, four rows a thread; then A and the rounding.  All loads of
+// added in a fixed order, four rows a thread, the parts' powers of two taken off; then
+// A and the rounding.  All loads of
 // other blocks are on their way before the first is added: one after the other, their
 // latency was up to half of a small product's time.
 template <typename OP, int PARTS, int SETS>
@@ -126,7 +130,11 @@ __device__ __forceinline__ void finish_tile(const ApplyArgs& a, const float* sum
         if (row0 + r >= a.m) continue;
         float sum[4] = {};
 #pragma unroll
-        for (int p = PARTS - 1; p >= 0; --p)                      // the smallest part first
+        for (int p = PARTS - 1; p >= 0; --p) {                    // the smallest part first
+            if (p < PARTS - 1) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] *= 1.f / kPartUp;
+            }
 #pragma unroll
             for (int s = 0; s < SETS; ++s) {
                 const float* at = sums + s * set + (v * PARTS + p) * pitch + r;
@@ -138,6 +146,7 @@ __device__ __forceinline__ void finish_tile(const ApplyArgs& a, const float* sum
                 for (int q = 0; q < 8; ++q)
                     if (q < a.split) sum[0] += w[q].x, sum[1] += w[q].y, sum[2] += w[q].z, sum[3] += w[q].w;
             }
+        }
         const int64_t o = (int64_t)(col0 / PARTS + v) * a.m + row0 + r;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
