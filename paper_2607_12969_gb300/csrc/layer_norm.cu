@@ -56,30 +56,12 @@ __device__ __forceinline__ void store8(bf16* p, const float (&v)[8]) {
                                               tc::pack_bf162(v[4], v[5]), tc::pack_bf162(v[6], v[7]));
 }
 
-// Two binary32 values as one operand of the two-lane instructions (half the
-// instructions of single ones: the gradient is bound by their number).
-using f2 = uint64_t;
-__device__ __forceinline__ f2 pair(float a, float b) {
-    f2 d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
-    return d;
-}
-__device__ __forceinline__ void split(f2 a, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a)); }
-__device__ __forceinline__ f2 add2(f2 a, f2 b) {
-    f2 d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
-    f2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
-    f2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
+using el::f2;
+using el::pair;
+using el::split;
+using el::add2;
+using el::mul2;
+using el::fma2;
 __device__ __forceinline__ float both_of(f2 a) {
     float x, y;
     split(a, x, y);
