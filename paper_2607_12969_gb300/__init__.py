@@ -18,6 +18,7 @@ lrc_tt_storage_bytes.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import NamedTuple, Optional, Sequence, Tuple
@@ -672,16 +673,29 @@ def lrc_distill_grad(Z, T, idx, w, lse, g, dZ, rows: int, V: int, K: int, ldz: i
 # convenience helpers built only from the entry points above
 # --------------------------------------------------------------------------
 
+def _on(stream, device):
+    """Torch's own work of a helper (copies, fills, the memory it allocates) goes
+    to the stream of the call: on another one a fill could come after the call
+    had written, and memory could still be in use there."""
+    if stream is None:
+        return contextlib.nullcontext()
+    cuda = _T().cuda
+    if isinstance(stream, int):
+        stream = cuda.ExternalStream(stream, device=device) if stream else cuda.default_stream(device)
+    return cuda.stream(stream)
+
+
 def round_matrix(src64, fmt, ld: Optional[int] = None, stream=None):
     """Round a 2-D CUDA float64 tensor into a new packed tensor (lrc_round_factors)."""
     import torch
     rows, cols = src64.shape
-    if src64.stride(1) != 1 or (rows > 1 and src64.stride(0) < cols):
-        src64 = src64.contiguous()
-    ld_src = src64.stride(0) if rows > 1 else cols   # a single row may carry any stride
     ld = lrc_packed_ld(cols) if ld is None else ld
-    dst = torch.empty((rows, ld), dtype=storage_dtype(fmt), device=src64.device)
-    lrc_round_factors(src64, rows, cols, ld_src, dst, ld, fmt, stream)
+    with _on(stream, src64.device):
+        if src64.stride(1) != 1 or (rows > 1 and src64.stride(0) < cols):
+            src64 = src64.contiguous()
+        ld_src = src64.stride(0) if rows > 1 else cols   # a single row may carry any stride
+        dst = torch.empty((rows, ld), dtype=storage_dtype(fmt), device=src64.device)
+        lrc_round_factors(src64, rows, cols, ld_src, dst, ld, fmt, stream)
     return dst
 
 
@@ -689,8 +703,9 @@ def widen_matrix(src, fmt, cols: int, stream=None):
     """Exact float64 copy (rows x packed ld) of a packed tensor (lrc_widen_factors)."""
     import torch
     rows, ld = src.shape
-    dst = torch.empty((rows, lrc_packed_ld(cols)), dtype=torch.float64, device=src.device)
-    lrc_widen_factors(src, fmt, rows, cols, ld, dst, dst.shape[1], stream)
+    with _on(stream, src.device):
+        dst = torch.empty((rows, lrc_packed_ld(cols)), dtype=torch.float64, device=src.device)
+        lrc_widen_factors(src, fmt, rows, cols, ld, dst, dst.shape[1], stream)
     return dst
 
 
@@ -711,11 +726,12 @@ def q4_matrix(W, fmt, group: int = 128, zeros: bool = False, stream=None) -> Q4M
     import torch
     wfmt = {torch.float64: "f64", torch.float32: "f32", torch.float16: "f16", torch.bfloat16: "bf16"}[W.dtype]
     m, n = W.shape
-    if W.stride(1) != 1 or (m > 1 and W.stride(0) < n):
-        W = W.contiguous()
     groups, ldm = (n + group - 1) // group, lrc_packed_ld(m)
-    Q = torch.empty((m, lrc_q4_row_bytes(n)), dtype=torch.uint8, device=W.device)
-    scales = torch.zeros((groups, ldm), dtype=storage_dtype(fmt), device=W.device)
-    z = torch.zeros((groups, ldm), dtype=torch.uint8, device=W.device) if zeros else None
-    lrc_q4_round(W, wfmt, m, n, W.stride(0) if m > 1 else n, Q, scales, z, group, fmt, stream)
+    with _on(stream, W.device):
+        if W.stride(1) != 1 or (m > 1 and W.stride(0) < n):
+            W = W.contiguous()
+        Q = torch.empty((m, lrc_q4_row_bytes(n)), dtype=torch.uint8, device=W.device)
+        scales = torch.zeros((groups, ldm), dtype=storage_dtype(fmt), device=W.device)
+        z = torch.zeros((groups, ldm), dtype=torch.uint8, device=W.device) if zeros else None
+        lrc_q4_round(W, wfmt, m, n, W.stride(0) if m > 1 else n, Q, scales, z, group, fmt, stream)
     return Q4Matrix(Q, scales, z, m, n, group, fmt)
