@@ -662,7 +662,7 @@ LRC_API lrc_status lrc_layer_norm_grad(const void* dY, const void* X, const void
  *           not wanted
  *   dZ      device, rows x V, row pitch lddz (>= V), Z's type; NULL where not
  *           wanted.  May be Z where the pitch is the same
- *   tau     > 0 and finite
+ *   tau     > 0 and finite, and log2(e) / tau too, in binary32
  *
  * A row without teacher entries, or with w = 0, has loss 0 and gradient 0,
  * whatever its logits are.  Logits of -infinity have q = 0 (a teacher entry

@@ -568,7 +568,7 @@ lrc_status check_distill(const void* Z, const void* T, const int64_t* idx, const
     if (!extent_ok(rows, ldz) || !extent_ok(rows, ldt) || (dZ && !extent_ok(rows, lddz))) return invalid("size overflow");
     const float t = (float)tau;
     if (!(t > 0.f) || isinf(t)) return invalid("tau = %g must be positive and finite in binary32", tau);
-    if (isinf(1.f / t)) return invalid("tau = %g is too small", tau);
+    if (isinf(1.4426950408889634f * (1.f / t))) return invalid("tau = %g is too small", tau);    // log2(e) / tau
     if (K > distill_max_top()) return unsupported("more than 1024 teacher entries a row");
     if (V > 1 << 30) return unsupported("more than 2^30 logits a row");
     if (rows == 0) return LRC_OK;
