@@ -127,7 +127,7 @@ struct Running {
 // What the teacher's warp leaves for a row.
 struct Teacher {
     float c;                 // tau w g, 0 where the row has no gradient
-    float lw;                // tau^2 w, 0 where the row has no loss
+    float lw;                // tau w, 0 where the row has no loss (tau^2 alone may leave binary32)
     int repeated;            // some place is named more than once
 };
 
@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_k
             if (lane == 0) {
                 const bool on = top != none && w != 0.f;
                 teacher[p].c = on && g != 0.f ? a.tau * w * g : 0.f;
-                teacher[p].lw = on ? a.tau * a.tau * w : 0.f;
+                teacher[p].lw = on ? a.tau * w : 0.f;
                 teacher[p].repeated = repeated;
             }
             __syncwarp();
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_k
                 }
                 kl = el::warp_sum(kl);
                 const float lw = teacher[ahead].lw;
-                if (lane == 0) a.loss[row] = lw != 0.f ? lw * kl : 0.f;
+                if (lane == 0) a.loss[row] = lw != 0.f ? lw * (a.tau * kl) : 0.f;
             }
             if (dZ) {
                 T* d = dZ + row * a.lddz;
