@@ -2,7 +2,7 @@
 // fifth-generation tensor cores (tcgen05, accumulators and the matrix in tensor
 // memory).
 //
-// A tile is 256 rows of the matrix and NC columns of vectors, 128 columns of the
+// A tile is 256 rows of the matrix and 64 columns of vectors, 128 columns of the
 // matrix (a block) at a time, brought by TMA.  Two pairs of teams of four warps take
 // every second block each, a team of a pair half of the rows: a thread unpacks its
 // row's 128 codes to the integers q - z, exact in 16 bits, and writes them to tensor
@@ -34,6 +34,7 @@ __device__ unsigned int g_err_q4_wide;
 
 constexpr int kPairs = 2, kTeams = 2 * kPairs, kTeamThreads = 128, kThreads = kTeams * kTeamThreads;
 constexpr int kRows = 256;
+constexpr int kCols = 64;                         // columns of vectors of a tile
 constexpr uint32_t kTmem = 512, kACols = 64;      // columns of tensor memory; of a team's A (128 x 128 of 16 bits)
 constexpr int kMostStages = 4;                    // of a pair
 
@@ -53,29 +54,27 @@ __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) 
 }
 
 // Shared memory of a stage, one block of 128 columns: kRows rows of 64 bytes of codes
-// (64-byte swizzle), two boxes of 64 columns of x (NC rows of 128 bytes, 128-byte
+// (64-byte swizzle), two boxes of 64 columns of x (kCols rows of 128 bytes, 128-byte
 // swizzle), scales and zero codes of the groups, kRows a group.
-template <typename S, int GROUP, bool ZEROS, int NC>
+template <typename S, int GROUP, bool ZEROS>
 struct WideStage {
-    static constexpr int kGroups = 128 / GROUP, kX = kRows * 64, kXBox = NC * 128, kScales = kX + 2 * kXBox;
+    static constexpr int kGroups = 128 / GROUP, kX = kRows * 64, kXBox = kCols * 128, kScales = kX + 2 * kXBox;
     static constexpr int kScaleBytes = kGroups * kRows * (int)sizeof(S), kZeros = kScales + kScaleBytes;
     static constexpr int kZeroBytes = ZEROS ? kGroups * kRows : 0;
     static constexpr int kPitch = (kZeros + kZeroBytes + 1023) / 1024 * 1024;
-    static constexpr int kSums = kPairs * NC * (kRows + 4) * 4;
+    static constexpr int kSums = kPairs * kCols * (kRows + 4) * 4;
     static constexpr int kRoom = (kSmemOfSm - 3072) / kPitch / kPairs;
     static constexpr int kDepth = kRoom < kMostStages ? kRoom : kMostStages;        // stages of a pair
     static_assert(kDepth >= 2 && kSums <= kPairs * kDepth * kPitch, "the sums lie in the ring");
 };
 
-template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NC>
+template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS>
 __global__ void __launch_bounds__(kThreads, 1)
 q4_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap xmap,
                const __grid_constant__ CUtensorMap smap, const __grid_constant__ CUtensorMap zmap,
                const __grid_constant__ ApplyArgs a, const uint32_t idesc) {
-    using St = WideStage<S, GROUP, ZEROS, NC>;
+    using St = WideStage<S, GROUP, ZEROS>;
     constexpr int kDepth = St::kDepth, kGroups = St::kGroups;
-    // sums of so many groups fit into a team's share of tensor memory at once
-    constexpr int kAtOnce = kGroups == 1 ? 1 : NC > 32 ? 1 : 2;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t full[kPairs][kDepth], empty[kPairs][kDepth], done[kTeams];
     __shared__ uint32_t tmem_slot;
@@ -83,7 +82,7 @@ q4_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     const int warp = threadIdx.x >> 5, team = warp >> 2, pair = team >> 1, half = team & 1;
     const int rank = blockIdx.x % a.split;
     const int64_t row0 = (int64_t)(blockIdx.x / a.split) * kRows;
-    const int col0 = blockIdx.y * used_cols(NC, PARTS);
+    const int col0 = blockIdx.y * used_cols(kCols, PARTS);
     const int mine = (int)((a.blocks - rank + a.split - 1) / a.split);       // blocks of columns
     uint8_t* base = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
     volatile int* abort = &abort_flag;
@@ -105,7 +104,7 @@ q4_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     tc::pdl_wait();
     tc::pdl_trigger();
 
-    float acc[NC] = {};
+    float acc[kCols] = {};
     uint8_t* ring = base + pair * kDepth * St::kPitch;
     // the pair's n-th block, block 2 n + pair of the tile's, into its stage
     auto issue = [&](int n) {
@@ -122,7 +121,7 @@ q4_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     {
         const int r = threadIdx.x & 127, row = half * 128 + r;   // lane of tensor memory, row of the tile
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;       // the warp's first lane, in bits 16 and up
-        const uint32_t ta = tmem + team * kACols, td = tmem + kTeams * kACols + team * (kAtOnce * NC);
+        const uint32_t ta = tmem + team * kACols, td = tmem + kTeams * kACols + team * kCols;
         const bool issuer = r == 0;
         const int swz = r >> 1 & 3;
         uint32_t round = 0;
@@ -158,7 +157,7 @@ q4_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             }
             tc::tmem_st_wait();
 #pragma unroll
-            for (int g0 = 0; g0 < kGroups; g0 += kAtOnce) {
+            for (int g = 0; g < kGroups; ++g) {
                 tc::tc_fence_before();
                 tc::named_bar_sync(1 + team, kTeamThreads);
                 if (issuer) {
@@ -166,19 +165,17 @@ q4_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                     const uint64_t x[2] = {tc::desc_sw128(tc::smem_u32(from + St::kX)),
                                            tc::desc_sw128(tc::smem_u32(from + St::kX + St::kXBox))};
 #pragma unroll
-                    for (int g = g0; g < g0 + kAtOnce; ++g)
-#pragma unroll
-                        for (int i = 0; i < GROUP / 16; ++i) {
-                            const int kk = g * (GROUP / 16) + i;  // step of 16 columns
-                            mma_ts(td + (g - g0) * NC, ta + 8 * kk, x[kk >> 2] + 2 * (kk & 3), idesc, i != 0);
-                        }
+                    for (int i = 0; i < GROUP / 16; ++i) {
+                        const int kk = g * (GROUP / 16) + i;      // step of 16 columns
+                        mma_ts(td, ta + 8 * kk, x[kk >> 2] + 2 * (kk & 3), idesc, i != 0);
+                    }
                     tc::mma_commit(&done[team]);
-                    if (g0 + kAtOnce >= kGroups) tc::mma_commit(&empty[pair][k % kDepth]);
+                    if (g + 1 == kGroups) tc::mma_commit(&empty[pair][k % kDepth]);
                 }
                 if ((warp & 3) == 0) tc::mbar_wait(&done[team], round & 1, abort, &g_err_q4_wide, 2u);
                 // The stage of the block before is free where both teams' products are done
                 // (their codes are in tensor memory).
-                if (fetcher && g0 == 0 && k > 0 && issued < blocks && !*abort) {
+                if (fetcher && g == 0 && k > 0 && issued < blocks && !*abort) {
                     tc::mbar_wait(&empty[pair][(k - 1) % kDepth], (k - 1) / kDepth & 1, abort, &g_err_q4_wide, 4u);
                     if (!*abort) issue(issued++);
                 }
@@ -188,15 +185,13 @@ q4_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 __syncwarp();
                 tc::tc_fence_after();
 #pragma unroll
-                for (int g = g0; g < g0 + kAtOnce; ++g)
+                for (int c = 0; c < kCols; c += 32) {
+                    uint32_t v[32];
+                    tc::tmem_ld32(td + lanes + c, v);
+                    tc::tmem_ld_wait();
 #pragma unroll
-                    for (int c = 0; c < NC; c += 32) {
-                        uint32_t v[32];
-                        tc::tmem_ld32(td + lanes + (g - g0) * NC + c, v);
-                        tc::tmem_ld_wait();
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) acc[c + i] = fmaf(s[g], __uint_as_float(v[i]), acc[c + i]);
-                    }
+                    for (int i = 0; i < 32; ++i) acc[c + i] = fmaf(s[g], __uint_as_float(v[i]), acc[c + i]);
+                }
             }
         }
         if (*abort && (issuer || fetcher)) {
@@ -213,20 +208,20 @@ q4_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     __syncwarp();
     if (warp == 0) tc::tmem_dealloc(tmem, kTmem);
     // sums[pair][column][row]
-    float(*sums)[NC][kRows + 4] = reinterpret_cast<float(*)[NC][kRows + 4]>(base);
+    float(*sums)[kCols][kRows + 4] = reinterpret_cast<float(*)[kCols][kRows + 4]>(base);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) sums[pair][c][threadIdx.x & (kRows - 1)] = acc[c];
+    for (int c = 0; c < kCols; ++c) sums[pair][c][threadIdx.x & (kRows - 1)] = acc[c];
     if (a.split > 1) cl::sync();
     else __syncthreads();
-    const int used = min(a.cols - col0, used_cols(NC, PARTS)) / PARTS;       // vectors of this tile
-    finish_tile<OP, PARTS, kPairs>(a, &sums[0][0][0], NC * (kRows + 4), kRows + 4, kRows, row0, col0, used, rank, kThreads);
+    const int used = min(a.cols - col0, used_cols(kCols, PARTS)) / PARTS;       // vectors of this tile
+    finish_tile<OP, PARTS, kPairs>(a, &sums[0][0][0], kCols * (kRows + 4), kRows + 4, kRows, row0, col0, used, rank, kThreads);
     if (a.split > 1) cl::sync();                                 // the sums stay until they are read
 }
 
-template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NC>
+template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS>
 lrc_status wide_as(ApplyArgs a, cudaStream_t s) {
-    using St = WideStage<S, GROUP, ZEROS, NC>;
-    constexpr int kUsed = used_cols(NC, PARTS);
+    using St = WideStage<S, GROUP, ZEROS>;
+    constexpr int kUsed = used_cols(kCols, PARTS);
     a.xrows = a.cols < kUsed ? a.cols : kUsed;
     const int chunks = (a.cols + kUsed - 1) / kUsed;
     const int64_t tiles = (a.m + kRows - 1) / kRows;
@@ -258,7 +253,7 @@ lrc_status wide_as(ApplyArgs a, cudaStream_t s) {
                            "zeros");
         if (st != LRC_OK) return st;
     }
-    auto kernel = q4_wide_kernel<OP, S, PARTS, GROUP, ZEROS, NC>;
+    auto kernel = q4_wide_kernel<OP, S, PARTS, GROUP, ZEROS>;
     constexpr int kSmem = kPairs * St::kDepth * St::kPitch + 1024;
     // the attribute is the device's: set once on each
     static std::atomic<uint64_t> set_on{0};
@@ -282,22 +277,10 @@ lrc_status wide_as(ApplyArgs a, cudaStream_t s) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = a.split > 1 ? 2 : 1;
-    const uint32_t idesc = tc::idesc_f16_f32(128, NC) | (OP::kBf16 ? tc::kIdescBF16 : 0u);
+    const uint32_t idesc = tc::idesc_f16_f32(128, kCols) | (OP::kBf16 ? tc::kIdescBF16 : 0u);
     e = cudaLaunchKernelEx(&cfg, kernel, qm, xm, sm, zm, a, idesc);
     if (e != cudaSuccess) return cuda_fail(e, "q4_wide_kernel");
     return after_launch("q4_wide_kernel");
-}
-
-template <typename OP, typename S, int PARTS, int NC>
-lrc_status wide_groups(const ApplyArgs& a, int group, cudaStream_t s) {
-    if (a.zeros) {
-        if (group == 32) return wide_as<OP, S, PARTS, 32, true, NC>(a, s);
-        if (group == 64) return wide_as<OP, S, PARTS, 64, true, NC>(a, s);
-        return wide_as<OP, S, PARTS, 128, true, NC>(a, s);
-    }
-    if (group == 32) return wide_as<OP, S, PARTS, 32, false, NC>(a, s);
-    if (group == 64) return wide_as<OP, S, PARTS, 64, false, NC>(a, s);
-    return wide_as<OP, S, PARTS, 128, false, NC>(a, s);
 }
 
 }  // namespace
@@ -306,8 +289,14 @@ namespace q4 {
 
 template <typename OP, typename S, int PARTS>
 lrc_status launch_wide(ApplyArgs a, int group, cudaStream_t s) {
-    return a.cols <= used_cols(32, PARTS) ? wide_groups<OP, S, PARTS, 32>(a, group, s)
-                                          : wide_groups<OP, S, PARTS, 64>(a, group, s);
+    if (a.zeros) {
+        if (group == 32) return wide_as<OP, S, PARTS, 32, true>(a, s);
+        if (group == 64) return wide_as<OP, S, PARTS, 64, true>(a, s);
+        return wide_as<OP, S, PARTS, 128, true>(a, s);
+    }
+    if (group == 32) return wide_as<OP, S, PARTS, 32, false>(a, s);
+    if (group == 64) return wide_as<OP, S, PARTS, 64, false>(a, s);
+    return wide_as<OP, S, PARTS, 128, false>(a, s);
 }
 template lrc_status launch_wide<Half2, __half, 1>(ApplyArgs, int, cudaStream_t);
 template lrc_status launch_wide<Bf2, bf16, 1>(ApplyArgs, int, cudaStream_t);
