@@ -80,7 +80,6 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = 2 * a.R, threads = 64 * a.R + 32;
     const int rows = 16 * a.R, rank = blockIdx.x % a.split;
     const int64_t row0 = (int64_t)(blockIdx.x / a.split) * rows;
-    const int col0 = blockIdx.y * used_cols(8 * NT, PARTS);
     const int stages = (int)((a.blocks + 3) / 4);
     const int mine = (stages - rank + a.split - 1) / a.split;         // stages of this block
     uint8_t* ring = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
@@ -113,7 +112,7 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                     tc::tma_load_2d(to + q * lay.codes, &qmap, unit * 256 + q * 128, (int32_t)row0, bar);
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
-                    tc::tma_load_2d(to + 2 * lay.codes + q * St::kXBox, &xmap, unit * 512 + q * 64, col0, bar);
+                    tc::tma_load_2d(to + 2 * lay.codes + q * St::kXBox, &xmap, unit * 512 + q * 64, 0, bar);
                 tc::tma_load_2d(to + lay.scales, &smap, (int32_t)row0, unit * St::kGroups, bar);
                 if (ZEROS) tc::tma_load_2d(to + lay.zeros, &zmap, (int32_t)row0, unit * St::kGroups, bar);
                 if (++slot == a.depth) {
@@ -214,8 +213,7 @@ q4_apply_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     }
     if (a.split > 1) cl::sync();
     else __syncthreads();
-    const int used = min(a.cols - col0, used_cols(8 * NT, PARTS)) / PARTS;      // vectors of this tile
-    finish_tile<OP, PARTS, 2>(a, sums, kCols * pitch, pitch, rows, row0, col0, used, rank, threads);
+    finish_tile<OP, PARTS, 2>(a, sums, kCols * pitch, pitch, rows, row0, 0, a.cols / PARTS, rank, threads);
     if (a.split > 1) cl::sync();                              // the sums stay until they are read
 }
 
@@ -249,11 +247,11 @@ q4_parts_kernel(const float* __restrict__ x, int64_t n, int64_t ldn, int64_t ldp
 // model of a multiprocessor's time, in units of what it takes for 16 rows and a
 // stage (0.11 us).  A block needs five such a stage at least however few its rows
 // are (the latency of its warps' chain), and sixteen to start and to end.
-inline void choose_tile(ApplyArgs* a, int chunks) {
+inline void choose_tile(ApplyArgs* a) {
     const int stages = (int)((a->blocks + 3) / 4), sms = sm_count();
     double best = 1e300;
     for (int R = kMostRows; R >= 1; --R) {
-        const int64_t tiles = ((a->m + 15) / 16 + R - 1) / R * chunks;
+        const int64_t tiles = ((a->m + 15) / 16 + R - 1) / R;
         const int slots = (R > 4 ? 1 : 2) * sms;
         for (int split = 1; split <= 8 && split <= stages; split += split < 4 ? 1 : 2) {
             const double blocks = (double)tiles * split;
@@ -271,10 +269,8 @@ inline void choose_tile(ApplyArgs* a, int chunks) {
 template <typename OP, typename S, int PARTS, int GROUP, bool ZEROS, int NT>
 lrc_status apply_launch(ApplyArgs a, cudaStream_t s) {
     using St = StageOf<S, GROUP, ZEROS, NT>;
-    constexpr int kUsed = used_cols(8 * NT, PARTS);
-    a.xrows = a.cols < kUsed ? a.cols : kUsed;
-    const int chunks = (a.cols + kUsed - 1) / kUsed;
-    choose_tile(&a, chunks);
+    a.xrows = a.cols;
+    choose_tile(&a);
     const uint32_t rows = 16 * a.R;
     const St lay(a.R);
     const int room = kSmemOfSm / (a.R > 4 ? 1 : 2) - 3072;
@@ -308,7 +304,7 @@ lrc_status apply_launch(ApplyArgs a, cudaStream_t s) {
     }
     if (e != cudaSuccess) return cuda_fail(e, "q4_apply_kernel");
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(grid, (unsigned)chunks);
+    cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(64 * a.R + 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
@@ -337,14 +333,12 @@ lrc_status apply_groups(const ApplyArgs& a, int group, cudaStream_t s) {
     return apply_launch<OP, S, PARTS, 128, false, NT>(a, s);
 }
 
-// The narrowest tiles of columns that take the vectors in as few passes over the
-// codes as the widest would.
+// As many tiles of eight columns as the vectors need.
 template <typename OP, typename S, int PARTS>
 lrc_status apply_tiles(const ApplyArgs& a, int group, cudaStream_t s) {
-    const int passes = (a.cols + used_cols(32, PARTS) - 1) / used_cols(32, PARTS);
-    if (used_cols(8, PARTS) * passes >= a.cols) return apply_groups<OP, S, PARTS, 1>(a, group, s);
-    if (used_cols(16, PARTS) * passes >= a.cols) return apply_groups<OP, S, PARTS, 2>(a, group, s);
-    if (used_cols(24, PARTS) * passes >= a.cols) return apply_groups<OP, S, PARTS, 3>(a, group, s);
+    if (a.cols <= 8) return apply_groups<OP, S, PARTS, 1>(a, group, s);
+    if (a.cols <= 16) return apply_groups<OP, S, PARTS, 2>(a, group, s);
+    if (a.cols <= 24) return apply_groups<OP, S, PARTS, 3>(a, group, s);
     return apply_groups<OP, S, PARTS, 4>(a, group, s);
 }
 
