@@ -246,7 +246,12 @@ q4_parts_kernel(const float* __restrict__ x, int64_t n, int64_t ldn, int64_t ldp
 // Groups of rows of a tile and blocks of a cluster: what takes the shortest by a
 // model of a multiprocessor's time, in units of what it takes for 16 rows and a
 // stage (0.11 us).  A block needs five such a stage at least however few its rows
-// are (the latency of its warps' chain), and sixteen to start and to end.
+// are (the latency of its warps' chain), and sixteen to start and to end.  It takes the
+// multiprocessors as one pool, although a cluster needs room in one part of them, and
+// counts two blocks of four groups of rows on each, although instances of more than 112
+// registers (three tiles of columns in part, four) have room for one there: 2254 x 3764
+// and 29 binary16 vectors take 16.6 us, with one counted 7.7, but 4446 x 13988 and 7
+// binary32 ones 25 and 32.
 inline void choose_tile(ApplyArgs* a) {
     const int stages = (int)((a->blocks + 3) / 4), sms = sm_count();
     double best = 1e300;
