@@ -141,9 +141,9 @@ __global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_k
     constexpr int kChunk = THREADS * 32;                      // bytes: two vectors a thread
     constexpr int kWarps = THREADS / 32, N = kVec<T>, kAhead = teachers(THREADS);
     extern __shared__ __align__(128) uint8_t ring[];
-    __shared__ uint64_t full[kMostChunks], empty[kMostChunks], tfull[kAhead], tempty[kAhead], got[2];
+    __shared__ uint64_t full[kMostChunks], empty[kMostChunks], tfull[kAhead], tempty[kAhead], got;
     __shared__ float part_m[2][kWarps], part_s[2][kWarps];    // [row parity][warp]
-    __shared__ float all_m[2][8], all_s[2][8];                // [row parity][block of the cluster]
+    __shared__ float all_m[8], all_s[8];                      // [block of the cluster]
     __shared__ Teacher teacher[kAhead];
     __shared__ int abort_flag;
     int* at = reinterpret_cast<int*>(ring + a.chunks * kChunk);          // [kAhead][K]
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_k
             tc::mbar_init(&tfull[p], 1);
             tc::mbar_init(&tempty[p], kWarps);
         }
-        for (int p = 0; p < 2; ++p) tc::mbar_init(&got[p], ranks);
+        tc::mbar_init(&got, ranks);
         tc::fence_barrier_init();
     }
     if (ranks > 1) cl::sync();                            // every block's barriers are there
@@ -298,17 +298,16 @@ __global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_k
             return (int)i;
         };
         int edge_at_next = edge_of(0, &edge_next);
-        // Each block gives its maximum and sum to every block of the cluster.  (One that
-        // gives those of row r + 2 has all of row r + 1, which the others gave after they
-        // had read those of row r.  And no block writes a gradient before all have their
-        // teacher's places' logits, which may lie where it is written.)
-        auto exchange = [&](int p, int r, float m, float s) {
+        // Each block gives its maximum and sum of the cluster's one row to every block of
+        // it.  (No block writes a gradient before all have their teacher's places' logits,
+        // which may lie where it is written.)
+        auto exchange = [&](float m, float s) {
             if (threadIdx.x < ranks) {
-                cl::store(&all_m[p][rank], threadIdx.x, m);
-                cl::store(&all_s[p][rank], threadIdx.x, s);
-                cl::arrive(&got[p], threadIdx.x);
+                cl::store(&all_m[rank], threadIdx.x, m);
+                cl::store(&all_s[rank], threadIdx.x, s);
+                cl::arrive(&got, threadIdx.x);
             }
-            cl::wait(&got[p], r >> 1 & 1, abort, &g_err_distill, 2u);
+            cl::wait(&got, 0, abort, &g_err_distill, 2u);
         };
         int ahead = -1;                      // the row's teacher entries
         uint32_t tphase = 1;
@@ -385,9 +384,9 @@ __global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_k
                 }
                 if (ranks > 1) {
                     tc::mbar_wait(&tfull[ahead], tphase, abort, &g_err_distill, 1u);
-                    exchange(p, r, all.m, all.s);
+                    exchange(all.m, all.s);
                     Running both;
-                    for (uint32_t i = 0; i < ranks; ++i) both.join(all_m[p][i], all_s[p][i], k2);
+                    for (uint32_t i = 0; i < ranks; ++i) both.join(all_m[i], all_s[i], k2);
                     all = both;
                 }
                 base = base_of(all.m);
@@ -397,7 +396,7 @@ __global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_k
             } else {
                 if (ranks > 1) {
                     tc::mbar_wait(&tfull[ahead], tphase, abort, &g_err_distill, 1u);
-                    exchange(p, r, 0.f, 0.f);
+                    exchange(0.f, 0.f);
                 }
                 const float L = __ldg(a.lse_in + row);
                 base = fmaxf(fminf(L * a.tau, 3.402823466e38f), -3.402823466e38f);
@@ -525,7 +524,8 @@ lrc_status distill_launch(Args a, int ranks, int resident, cudaStream_t s) {
 
 template <typename T>
 lrc_status distill_as(Args a, cudaStream_t s) {
-    // Few rows: a cluster of up to eight blocks each, of 4096 elements at least.
+    // Few rows: a cluster of up to eight blocks each (a block for every multiprocessor at
+    // most, so that each cluster has one row), of 4096 elements at least.
     // (Clusters for rows that no block can keep are slower than reading them twice, the
     // second time from L2: 215 us against 133 for 512 rows of 262144 bfloat16.)
     int ranks = 1;
