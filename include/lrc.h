@@ -579,11 +579,13 @@ LRC_API lrc_status lrc_q4_widen(const void* Q, const void* scales, const uint8_t
  *
  * Element types of X and Y as in lrc_apply (LRC_F32, LRC_F32_TC: binary32;
  * LRC_F16: binary16 and binary32; LRC_F16_O16, LRC_BF16: 16 bits both); X, A
- * and Y 16-byte aligned.  Products with the integers code - zero are exact and
- * are summed in binary32 over at most a group of columns; each such sum is
- * scaled and added in binary32; A is added and the result rounded to Y's type
- * once.  (A group's sum comes before its scale: entries of X above 2^115 could
- * overflow there.)  Deterministic.  Made for the few vectors of a serving step:
+ * and Y 16-byte aligned.  Products with the integers code - zero are exact; they
+ * are summed over at most a group of columns by the matrix instructions, in
+ * binary32 but cut off, not rounded; each such sum is scaled and added in
+ * binary32; A is added and the result rounded to Y's type once.  Before that
+ * rounding Y is within 2^-23 (group + ceil(n / group) + 40) (|A| + |X| |What|^T)
+ * of the exact result.  (A group's sum comes before its scale: entries of X above
+ * 2^115 could overflow there.)  Deterministic.  Made for the few vectors of a serving step:
  * the weights are read once for up to 64 of them, 21 in binary32.  A binary32 X
  * is split into three bfloat16 parts in the stream's workspace (see lrc_apply),
  * 6 bytes an element, at most 256 MB of them, or one vector's, at a time (a
@@ -668,7 +670,12 @@ LRC_API lrc_status lrc_layer_norm_grad(const void* dY, const void* X, const void
  * whatever its logits are.  Logits of -infinity have q = 0 (a teacher entry
  * there makes the loss infinite); a row that has only those, or a NaN or
  * +infinity, gives NaN.  All pointers are aligned to their element size.
- * Z is read from memory once.  Arithmetic is binary32; dZ is rounded once.
+ * Z is read once where a row (of a few rows, a block's share of it) fits into a
+ * multiprocessor's shared memory, about 200 KB, or no gradient is asked for; else
+ * twice, the second time from the L2 as far as the rows at work fit there.
+ * Arithmetic is binary32, on differences from the row's largest logit, so that an
+ * offset of all of them (or of the teacher's) adds error to lse alone; dZ is
+ * rounded once.
  * LRC_F64 is LRC_ERR_UNSUPPORTED.  rows = 0: nothing is launched.
  * Deterministic.  Asynchronous on `stream`.
  */
@@ -678,7 +685,8 @@ LRC_API lrc_status lrc_distill(const void* Z, const void* T, const int64_t* idx,
 
 /*
  * lrc_distill_grad -- the gradient apart, for a program that has the loss
- * already: dz_j as above times g, from the lse that lrc_distill gave.
+ * already: dz_j as above times g, from the lse that lrc_distill gave (whose
+ * rounding, up to 2^-24 |lse|, is then one relative error of a row's q_j).
  *
  *   lse     device, rows binary32 values
  *   g       device, rows binary32 upstream gradients of the losses; NULL for

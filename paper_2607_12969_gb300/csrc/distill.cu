@@ -10,19 +10,22 @@
 // term, by 4e-5 of it for logits near 1000, and m k leaves binary32 for a row of the
 // lowest number.
 //
-// Bound by HBM (a row is read once and its gradient written once) and, with both
-// the sum and the gradient, nearly by the exponentials, two an element at 16 a
-// clock on a multiprocessor: 4096 rows of 65536 bfloat16 199 us, 5.4 TB/s; the
-// gradient alone for 1021 rows of 50001 binary16 35 us, 5.9 TB/s.  A few rows wait
-// for a chain of loads and the call: 16 of 32768 binary32 8 us.
+// Long rows are bound by HBM (a row read once, its gradient written once): 4096 rows
+// of 65536 bfloat16 199 us, 5.4 TB/s; the gradient alone for 1021 rows of 50001
+// binary16 35 us, 5.9 TB/s.  Shorter ones, and the forward pass, by the end of each row
+// (the block's maximum and sum, the logarithm, the loss, the teacher's places), when
+// most of the block waits: 2048 x 32768 bfloat16 forward 38 us (floor 20), 4096 x 8192
+// binary16 37 with the gradient (20).  Rows that do not fit into the ring are read
+// twice, from the L2 as far as the rows at work fit there: 512 x 262144 bfloat16 133
+// us, 256 of binary32 132 (floors 79).  A few rows wait for a chain of loads and the
+// call: 16 of 32768 binary32 8 us.
 //
 // Persistent blocks, one row at a time (or a cluster a row where rows are few, each
 // block a slice).  One warp brings the row in chunks by bulk copies into a ring in
 // shared memory, a few prepare the next rows' teacher entries (a row each: a chain of
 // two loads from memory and a softmax, longer than many a row's copies), the others
 // form the running maximum and sum chunk by chunk as they come and, where the row
-// fits into the ring, the gradient from the same copy; else the chunks come again
-// (from L2).  The ring holds the next row's first chunks by then.  At the places of
+// fits into the ring, the gradient from the same copy; else the chunks come again.  The ring holds the next row's first chunks by then.  At the places of
 // the teacher's entries the gradient is written once more at the end of the row.
 #include <math.h>
 
@@ -445,7 +448,8 @@ __global__ void __launch_bounds__(all_threads(THREADS), 512 / THREADS) distill_k
                         }
                     }
                     if (!same) {
-                        // a warp's vectors side by side, element by element
+                        // a warp's vectors side by side, element by element (1021 x 50001
+                        // binary16 and its gradient 66 us, where both start alike 54)
                         __syncwarp();
                         const T* from = reinterpret_cast<const T*>(v);
 #pragma unroll

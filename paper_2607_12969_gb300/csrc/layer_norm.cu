@@ -5,8 +5,10 @@
 //   dx = r (d - mean(d) - xh mean(d xh)),  d = dy gamma,  xh = (x - mu) r
 //   dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy
 //
-// Both are bound by HBM: every row is read once and held on chip between its
-// sums and its result (in registers, in the gradient also in shared memory).
+// Up to 32768 columns (the gradient 65536) a row is read once and held on chip
+// between its sums and its result, in registers, where rows are many first in shared
+// memory; longer rows are read three times.  HBM is the floor; what keeps each kernel
+// from it stands at the kernel.
 #include <type_traits>
 
 #include "cluster.cuh"
@@ -170,7 +172,10 @@ template <typename T> __device__ __forceinline__ void get(const Held<T>& h, floa
 // a warp takes a row), VPT groups of eight elements a thread.  One barrier: with
 // m_i the mean and q_i the sum of squares about it of the n_i elements of a part,
 // the whole has q = sum_i (q_i + n_i (m_i - m)^2), first over the lanes of a warp,
-// then over the warps.
+// then over the warps.  A few hundred rows wait for the call (64 x 8192 of binary16 7
+// us).  Six blocks of 256 threads and 16-bit rows on a multiprocessor: rows that start
+// anywhere spill 48 to 80 bytes a thread for it, 400 x 4097 9.9 us against 11.1 with
+// four blocks, but 8191 x 511 13.7 and 13.1, 500 x 7001 19.5 and 13.4.
 template <typename X, typename Y, bool VEC, int VPT, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : sizeof(X) == 2 ? 6 : 4) norm_kernel(const NormArgs a) {
     __shared__ float sh[2][32];
@@ -529,7 +534,7 @@ norm_stream_kernel(const __grid_constant__ NormArgs a, const int depth) {
 }
 
 // Rows too long for the registers of a block: read three times (from L2 after the
-// first).
+// first): 2048 x 40000 of bfloat16 160 us.
 template <typename X, typename Y>
 __global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs a) {
     __shared__ float sh[2][32];
@@ -580,9 +585,11 @@ constexpr int kGradThreads = 512;            // of a block, at most
 // warp has met at the row's barrier; a row is in registers (as xh and d) while its
 // two sums are added over the block and the cluster.  gamma is in shared memory,
 // and one thread asks for the copies.
-// What bounds it (8192 x 8192 of bfloat16, 81 us, 5.0 TB/s of 6.8): instructions, and
-// the chain of a row's sums; 1024 threads with eight columns each take 121 us, 256
-// with 32 91 (sixteen in single arithmetic: 120).  Rows that start
+// What bounds it (8192 x 8192 of bfloat16, 80 us, 5.0 TB/s of 6.8): the chain of a
+// row's sums, with one row of 16 warps at a time (1.75 instructions a cycle, no pipe
+// above 20 %); 1024 threads with eight columns each take 121 us, 256 with 32 91
+// (sixteen in single arithmetic: 120).  More than 8192 columns add the cluster's
+// exchange to every row's chain: 4096 x 16384 150 us.  Rows that start
 // anywhere pass element by element: 8191 x 4097 131 us against 49 for 8192 x 4096
 // (results by way of shared memory, as in norm_stream_kernel: 125, but 28 against 25
 // for 4099 x 1138 of binary32).
@@ -817,7 +824,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_kernel(const __grid
     if (ranks > 1) cl::sync();           // no block ends before the others have given it theirs
 }
 
-// Rows too long for that: dx a row a block, the columns' sums apart.
+// Rows too long for that: dx a row a block, the columns' sums apart (1000 x 70000 of
+// bfloat16 548 us).
 template <typename X, typename Y>
 __global__ void __launch_bounds__(1024) norm_grad_long_kernel(const GradArgs a) {
     __shared__ float sh[2][32];

@@ -33,10 +33,12 @@ using namespace q4;
 // blocks of a cluster share the columns of a tile; their sums are added in the
 // order of their ranks through distributed shared memory.
 //
-// What bounds it: the unpacking, 11 (bfloat16) or 9 (binary16) instructions for
-// eight codes, 7 or 5 of them on the pipe of half rate; and HBM.  16384 x 16384 and
-// one bfloat16 vector take 28 us, 4.8 TB/s of 6.8; 16384 x 8192 and 32 binary16
-// vectors 30 us.  A ring for each warp 39 us; loads to registers, whose x of L1
+// What bounds it: 16384 x 16384 and one bfloat16 vector take 28 us, 4.9 TB/s of 6.8,
+// with no unit full: the unpacking, 11 (binary16 9) instructions for eight codes, 7 (5)
+// of them on the pipe of half rate, is 55 % of that pipe's time, HBM 57 %; what is
+// missing is overlap of the two, with one block a multiprocessor.  With more vectors
+// every warp reads the block's x for its own 16 rows: 16384 x 8192 and 32 binary16
+// vectors 30 us, 12287 x 16381 and 7 binary32 ones (21 columns) 40.  A ring for each warp 39 us; loads to registers, whose x of L1
 // come in order behind the codes of memory, slower still; one run of stages for each
 // resident block, joined by counters, 34.
 
@@ -349,9 +351,10 @@ lrc_status apply_tiles(const ApplyArgs& a, int group, cudaStream_t s) {
 
 // Columns up to which the product is mma.sync's.  Either way one pass over the codes;
 // this one's warps hand nothing on, so it starts sooner: 1000 x 4000 and 30 bfloat16
-// vectors 7.4 us here, 11.2 on tcgen05; 12287 x 16381 and 10 binary32 vectors (30
-// columns) 50 and 76; 16384 x 8192 and 32 binary16 vectors 29.9 and 27.2.  Above, this
-// one would pass over the codes again: 48 vectors 52 us here, 32 there.
+// vectors 7.0 us here, 11.4 on tcgen05; 12287 x 16381 and 10 binary32 vectors (30
+// columns) 49 and 91; 16384 x 8192 and 32 binary16 vectors 30.1 and 30.4, 4096 x 4096
+// 14.9 and 11.4.  Above, this one would pass over the codes again: 48 vectors 52 us
+// here, 32 there.
 constexpr int kFew = 32;
 
 template <typename OP, typename S, typename Y, int PARTS>

@@ -18,7 +18,10 @@
 // flight -- all of tensor memory is in use -- and the polling of those who wait;
 // leaving out any one step of it gains 1 to 7 us.  With 128 rows a tile (34 us) the
 // vectors pass the multiprocessors' L2 ports twice as often: 128 vectors 65 us
-// against 56.  Four kinds of warps that hand blocks on took 57 us.
+// against 56.  Four kinds of warps that hand blocks on took 57 us.  Smaller groups are
+// multiplied, read and scaled one after the other: 38 us with groups of 64, 52 of 32,
+// whose four scales a thread also spill (28 to 56 bytes).  More than 64 vectors take
+// the codes again for every 64: 128 56 us, 2048 740.
 #include "q4.cuh"
 
 #include <math.h>
